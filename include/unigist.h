@@ -55,8 +55,8 @@ typedef enum {
  * Element types.  UNIGIST_E4M3 (one byte: E4M3 of the OCP 8-bit floating point format, bias 7, no infinities,
  * largest magnitude 448) is a storage type of the compressed cache only: unigist_quantize_e4m3 produces it, the
  * cache maintenance calls (unigist_cache_update, _ex, _ragged, unigist_cache_to_ring / _from_ring / _ring_append)
- * move it, unigist_decode_e4m3 and unigist_prefill_chunk_e4m3 read it; every other call answers
- * UNIGIST_EUNSUPPORTED to it.
+ * move it, unigist_decode_e4m3 and unigist_prefill_chunk_e4m3 read it, the unigist_paged_* calls do all three on their
+ * pages; every other call answers UNIGIST_EUNSUPPORTED to it.
  */
 typedef enum { UNIGIST_BF16 = 0, UNIGIST_F32 = 1, UNIGIST_E4M3 = 2 } unigist_dtype;
 
@@ -472,6 +472,85 @@ unigist_status unigist_prefill_chunk_ragged(const void* q, const void* kc, const
                                             int B, int Hq, int Hkv, int C, int D, int r, int W, int sinks,
                                             int window_mode, const int* p0, const int* n, const int* s, int cap,
                                             int* rows_out, unigist_dtype dt, void* hip_stream);
+
+/*
+ * A cache in pages: the rows of many sequences in one pool, shared out in pages, for batches that grow at different
+ * rates and mix prompts, drafts and single tokens (Sec. 4.3 serves one sequence from one slab).
+ *
+ * k, v: [n_pages, Hkv, page, D] (UNIGIST_BF16, or UNIGIST_E4M3 with element = code * scale of its kv head).  Row j of
+ * sequence b is slot j % page of page table[b][j / page]; a slab [B, Hkv, cap, D] is such a pool with page = cap and
+ * table[b] = {b}.  Any page size.  A table entry outside 0 .. n_pages - 1 is a page that is not there: its rows
+ * are seen by no query and written by no call.  Sequences may share pages for reading; rows that a call writes
+ * (unigist_paged_append, weights, the destination of unigist_paged_evict) belong to one sequence each.
+ * weight: a number per row and kv head, of the caller's (null where it is not asked for).
+ * k and v are 16-byte aligned, n_pages * Hkv * page below 2^31 rows and at most 64 GiB each (UNIGIST_EUNSUPPORTED
+ * otherwise).  The struct is read
+ * before a call returns.
+ */
+typedef struct unigist_paged_cache {
+    void* k;               /* DEVICE [n_pages, Hkv, page, D] */
+    void* v;
+    const float* k_scale;  /* DEVICE [Hkv], UNIGIST_E4M3 only */
+    const float* v_scale;
+    float* weight;         /* DEVICE [n_pages, Hkv, page], may be null */
+    const int* table;      /* DEVICE [B, table_cols] */
+    int n_pages, page, table_cols;
+    int Hkv, D;
+    unigist_dtype dt;
+} unigist_paged_cache;
+
+/*
+ * The batch that the calls below work on: T new rows, those of sequence b are the rows cu[b] .. cu[b+1]-1 of the new
+ * tensors and the last of its kv_len[b] rows (DEVICE arrays of B + 1 and B ints; cu null: one row a sequence, T = B).
+ * Neither is seen by the host.  kv_len outside 0 .. max_kv (2^23 where a call has no max_kv) and cu outside 0 .. T are
+ * taken as the nearest of these; cu has to be non-decreasing.  Rows of the new tensors behind cu[B] are left as they are.
+ *
+ * unigist_paged_append writes the new rows into their pages: element (h, t, d) of k_new and v_new (bf16, DEVICE) lies at
+ * h * head_stride + t * row_stride + d (multiples of 8, row_stride >= D, 16-byte aligned).  bf16 rows are copied, codes
+ * are made as unigist_quantize_e4m3 makes them; the weight of a new row, where there are weights, becomes 0.  Rows whose
+ * page is not there are dropped.
+ */
+unigist_status unigist_paged_append(const unigist_paged_cache* cache, const void* k_new, const void* v_new,
+                                    long long head_stride, long long row_stride, int B, int T, const int* cu,
+                                    const int* kv_len, void* hip_stream);
+
+/*
+ * Attention of the new rows, whose keys the pages hold already: new row i of sequence b is position
+ * p = kv_len[b] - n[b] + i (n[b] = cu[b+1] - cu[b]) and sees row j <= p by the rule of unigist_attn_fwd_ex with r, W, sinks,
+ * window_mode (W >= max_kv in the sliding mode: plain causal attention), positions being row numbers.  A new row
+ * that sees nothing gets out = 0 and lse = -inf; what invisible rows hold, infinities and NaN included, enters no result.
+ * q, out: bf16, element (h, t, d) at h * q_head_stride + t * q_row_stride + d (as for append); lse [Hq, T] float, may be null.
+ * max_new >= every n[b] and max_kv >= every kv_len[b] choose the launch; rows of a sequence with more new ones may be left
+ * unwritten.
+ *
+ * weigh > 0 (needs cache->weight and lse): for every row j < kv_len[b] of every sequence with new rows, and every kv head,
+ *   weight[j] = decay * weight[j] + sum over the last min(weigh, n[b]) new rows i and the query heads of the group
+ *               that see j of exp(score_ij - lse_i)
+ * -- the attention that the row received; decay = 1 adds up, decay = 0 overwrites whatever was there.  The sums are in a fixed order.
+ * workspace: unigist_paged_attn_workspace(...) bytes for the same arguments (0: invalid), 256-byte aligned, contents undefined
+ * on entry and exit.
+ */
+unigist_status unigist_paged_attn(const unigist_paged_cache* cache, const void* q, void* out, float* lse, int B, int Hq,
+                                  int T, const int* cu, const int* kv_len, int max_new, int max_kv, int r, int W,
+                                  int sinks, int window_mode, long long q_head_stride, long long q_row_stride, int weigh,
+                                  float decay, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t unigist_paged_attn_workspace(const unigist_paged_cache* cache, int B, int Hq, int T, int max_new, int max_kv, int r,
+                                    int W, int sinks, int window_mode, int weigh);
+
+/*
+ * Eviction by weight: of the kv_len[b] rows of sequence b, every kv head keeps keep[b] (all, if there are no more) and
+ * copies them, in order, to the rows 0, 1, .. of sequence b in `dst`, with their weights where dst has them.  First in are
+ * the protected rows, the first `sinks` and the last `recent`, then the others by weight, largest first (NaN below
+ * every number); of equal ones the lower row.
+ * dst: the same pool under another table, or another pool (any page size; Hkv, D and dt of src); its pages are none of
+ * those that src's tables name.  src is left as it is.
+ * kv_len, keep: DEVICE, B ints, kv_len[b] <= max_kv, keep[b] <= max_keep.  kept (DEVICE [B, Hkv, max_keep], out): the rows
+ * kept, ascending, then -1.  rows_out (DEVICE, B ints, out; not kv_len's or keep's memory): rows kept, or -1 for a sequence whose numbers are outside those
+ * bounds or that misses a page on either side; nothing is copied for it and its part of kept is all -1.
+ */
+unigist_status unigist_paged_evict(const unigist_paged_cache* src, const unigist_paged_cache* dst, int B, const int* kv_len,
+                                   const int* keep, int max_kv, int max_keep, int sinks, int recent, int* kept,
+                                   int* rows_out, void* hip_stream);
 
 /*
  * Block map (Sec. 4.2: with a fixed compression ratio the visible blocks are known in

@@ -37,6 +37,7 @@ EXPORTS = [
     "unigist_decode_noalloc", "unigist_decode_noalloc_scratch_bytes", "unigist_debug_force_plain_alu",
     "unigist_window_start", "unigist_plan_row_tile", "unigist_plan_row_group", "unigist_plan_row_slot", "unigist_bwd_plan_build", "unigist_plan_key_tile", "unigist_plan_gist_unit",
     "unigist_probe_read_rate",
+    "unigist_paged_append", "unigist_paged_attn", "unigist_paged_attn_workspace", "unigist_paged_evict",
 ]
 
 
@@ -65,6 +66,11 @@ class _BwdPlan(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("key_tile", "chunk_rows", "n_chunks", "n_key_tiles", "n_gist_tiles", "seg_chunks",
                                        "n_segs")] + [("slot0", C.c_int * 33)] + \
                [(n, C.c_size_t) for n in ("partial_bytes", "reduced_bytes", "workspace_bytes")]
+
+
+class _PagedCache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "weight", "table")] + \
+               [(n, C.c_int) for n in ("n_pages", "page", "table_cols", "Hkv", "D", "dt")]
 
 
 def lib_path() -> str:
@@ -190,6 +196,16 @@ def load():
     lib.unigist_probe_read_rate.argtypes = [vp, sz, vp, ip, vp]
     lib.unigist_probe_mfma_rate.restype = ip
     lib.unigist_probe_mfma_rate.argtypes = [vp, vp, vp, ip, ip, vp]
+    pcp = C.POINTER(_PagedCache)
+    lib.unigist_paged_append.restype = ip
+    lib.unigist_paged_append.argtypes = [pcp, vp, vp, C.c_longlong, C.c_longlong, ip, ip, vp, vp, vp]
+    lib.unigist_paged_attn.restype = ip
+    lib.unigist_paged_attn.argtypes = [pcp, vp, vp, fp, ip, ip, ip, vp, vp] + [ip] * 6 + [C.c_longlong] * 2 + \
+        [ip, C.c_float, vp, sz, vp]
+    lib.unigist_paged_attn_workspace.restype = sz
+    lib.unigist_paged_attn_workspace.argtypes = [pcp] + [ip] * 10
+    lib.unigist_paged_evict.restype = ip
+    lib.unigist_paged_evict.argtypes = [pcp, pcp, ip, vp, vp] + [ip] * 4 + [vp, vp, vp]
     lib.unigist_tile_sizes.restype = None
     lib.unigist_tile_sizes.argtypes = [ip, ip, C.POINTER(ip), C.POINTER(ip)]
     _LIB = lib
@@ -591,6 +607,25 @@ def probe_mfma_rate(operands, blocks=512, iters=100000):
     flops = blocks * 4 * iters * 8 * 2.0 * 32 * 32 * 16
     c = clocks.view(blocks, 2).sum(0).tolist()
     return flops / e0.elapsed_time(e1) / 1e9, 100.0 * c[0] / max(c[1], 1)
+
+
+def unigist_paged_append(cache, k_new, v_new, head_stride, row_stride, B, T, cu, kv_len, stream=None) -> int:
+    """cache: a _PagedCache (see _paged_cache), like in the next three."""
+    return load().unigist_paged_append(cache, k_new, v_new, head_stride, row_stride, B, T, cu, kv_len, stream)
+
+
+def unigist_paged_attn(cache, q, out, lse, B, Hq, T, cu, kv_len, max_new, max_kv, r, W, sinks, window_mode, q_hs, q_rs, weigh,
+                       decay, ws, ws_bytes, stream=None) -> int:
+    return load().unigist_paged_attn(cache, q, out, lse, B, Hq, T, cu, kv_len, max_new, max_kv, r, W, sinks, window_mode, q_hs,
+                                     q_rs, weigh, decay, ws, ws_bytes, stream)
+
+
+def unigist_paged_attn_workspace(cache, B, Hq, T, max_new, max_kv, r, W, sinks, window_mode, weigh) -> int:
+    return load().unigist_paged_attn_workspace(cache, B, Hq, T, max_new, max_kv, r, W, sinks, window_mode, weigh)
+
+
+def unigist_paged_evict(src, dst, B, kv_len, keep, max_kv, max_keep, sinks, recent, kept, rows_out, stream=None) -> int:
+    return load().unigist_paged_evict(src, dst, B, kv_len, keep, max_kv, max_keep, sinks, recent, kept, rows_out, stream)
 
 
 def unigist_tile_sizes(D, dt):
@@ -1097,3 +1132,139 @@ def prefill_chunk(q, cache: "KVCache", r, W, p0, window_mode=UNIGIST_WINDOW_SLID
                                     int(window_mode), int(p0), cache.s, cache.cap, _dt(q), _stream()),
            "unigist_prefill_chunk_ex")
     return out, lse
+
+
+# ---------------------------------------------------------------- caches in pages
+def _paged_cache(k, v, table, k_scale, v_scale, weight, values=True):
+    """The descriptor of a pool k, v [n_pages, Hkv, page, D] (bf16, or uint8 codes, with scales where values are read or
+    written) and a table int32 [B, cols]."""
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+        raise UnigistError("k and v must be pools [n_pages, Hkv, page, D] of one shape and dtype")
+    if k.dtype == torch.uint8:
+        dt = UNIGIST_E4M3
+        if values:
+            if k_scale is None or v_scale is None:
+                raise UnigistError("pages of E4M3 codes need k_scale and v_scale")
+            _scales(k_scale, k.shape[1])
+            _scales(v_scale, k.shape[1])
+    elif k.dtype == torch.bfloat16:
+        dt, k_scale, v_scale = UNIGIST_BF16, None, None
+    else:
+        raise UnigistError(f"unsupported dtype {k.dtype}: pages hold bf16 or uint8 (E4M3 codes)")
+    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[1] < 1:
+        raise UnigistError("table must be int32 [B, cols]")
+    if weight is not None and (weight.dtype != torch.float32 or weight.shape != k.shape[:3]):
+        raise UnigistError("weight must be float32 [n_pages, Hkv, page]")
+    _dev(k, v, table, weight)
+    n_pages, Hkv, page, D = k.shape
+    return _PagedCache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+                       None if v_scale is None else v_scale.data_ptr(), None if weight is None else weight.data_ptr(),
+                       table.data_ptr(), n_pages, page, table.shape[1], Hkv, D, dt)
+
+
+def _int32(t, n, what):
+    if t.dtype != torch.int32 or t.shape != (n,) or not t.is_cuda or not t.is_contiguous():
+        raise UnigistError(f"{what} must be int32 [{n}] on the GPU")
+    return t.data_ptr()
+
+
+def _rows_view(t, what):
+    """t [H, T, D] bf16, or a contiguous copy where its rows are not apart from each other in steps of 16 bytes, and its
+    (head, row) strides."""
+    if not t.is_cuda:
+        raise UnigistError("libunigist takes device tensors only (no CPU path)")
+    if t.dtype != torch.bfloat16:
+        raise UnigistError(f"{what} must be bf16")
+    H, T, D = t.shape
+    if H == 0:
+        raise UnigistError(f"{what} has no heads")
+    hs, rs, es = t.stride()
+    hs, rs = (hs if H > 1 else T * D), (rs if T > 1 else D)  # the stride of an axis of one entry may be any number
+    apart = rs >= D and hs >= D and (hs >= (T - 1) * rs + D or rs >= (H - 1) * hs + D or T <= 1)
+    if (es != 1 and D > 1) or hs % 8 or rs % 8 or not apart or t.data_ptr() % 16:
+        t = t.contiguous()
+        if t.data_ptr() % 16:
+            t = t.clone()
+        hs, rs = T * D, D
+    return t, hs, rs
+
+
+def _same_device(*ts):
+    for t in ts:
+        if t is not None and t.device != ts[0].device:
+            raise UnigistError("tensors must be on one device")
+
+
+def paged_append(k, v, table, kv_len, k_new, v_new, cu=None, k_scale=None, v_scale=None, weight=None):
+    """Write the new rows k_new, v_new [Hkv, T, D] (bf16; views such as the transposed one of [T, Hkv, D] are taken
+    as they are) into the pages of a pool k, v
+    [n_pages, Hkv, page, D] (bf16, or uint8: quantised with k_scale, v_scale).  Sequence b's are the rows cu[b] .. cu[b+1]-1
+    (cu int32 [B+1] on the GPU; None: one each) and become the last of its kv_len[b] rows (int32 [B] on the GPU); their
+    weights become 0."""
+    c = _paged_cache(k, v, table, k_scale, v_scale, weight)
+    B = table.shape[0]
+    if k_new.dim() != 3 or k_new.shape[0] != c.Hkv or k_new.shape[2] != c.D or v_new.shape != k_new.shape:
+        raise UnigistError("k_new and v_new must be [Hkv, T, D]")
+    T = k_new.shape[1]
+    _same_device(k, v, table, kv_len, k_new, v_new, cu, k_scale, v_scale, weight)
+    k_new, hs, rs = _rows_view(k_new, "k_new")
+    v_new, vhs, vrs = _rows_view(v_new, "v_new")
+    if (vhs, vrs) != (hs, rs):
+        k_new, hs, rs = _rows_view(k_new.contiguous(), "k_new")
+        v_new = _rows_view(v_new.contiguous(), "v_new")[0]
+    _check(unigist_paged_append(C.byref(c), k_new.data_ptr(), v_new.data_ptr(), hs, rs, B, T,
+                                None if cu is None else _int32(cu, B + 1, "cu"), _int32(kv_len, B, "kv_len"), _stream()),
+           "unigist_paged_append")
+
+
+def paged_attn(q, k, v, table, kv_len, r, W, cu=None, max_new=None, max_kv=None, sinks=0, window_mode=UNIGIST_WINDOW_SLIDING,
+               k_scale=None, v_scale=None, weight=None, weigh=0, decay=1.0, workspace=None):
+    """Attention of the new rows q [Hq, T, D] (bf16; views such as the transposed one of [T, Hq, D] are taken as they are)
+    over a pool of pages that holds their keys already -> out [Hq, T, D] in the same layout, lse [Hq, T].  cu, kv_len: see paged_append.  r, W, sinks, window_mode: the mask of
+    attn_fwd over row numbers; W >= max_kv is plain causal attention.  max_new, max_kv: the most new rows and rows of any sequence
+    (None: whatever the tensors allow; the closer they are, the better the launch fits).  weigh > 0: `weight` (float32
+    [n_pages, Hkv, page]) becomes decay * weight + the attention each row received from the last `weigh` new rows of its
+    sequence.  workspace: a uint8 tensor to reuse, optional."""
+    c = _paged_cache(k, v, table, k_scale, v_scale, weight)
+    B = table.shape[0]
+    if q.dim() != 3 or q.shape[2] != c.D:
+        raise UnigistError("q must be [Hq, T, D]")
+    Hq, T, D = q.shape
+    _same_device(k, v, table, kv_len, q, cu, k_scale, v_scale, weight, workspace)
+    q, hs, rs = _rows_view(q, "q")
+    max_new = (1 if cu is None else max(T, 1)) if max_new is None else int(max_new)
+    max_kv = min(c.table_cols * c.page, 1 << 23) if max_kv is None else int(max_kv)
+    sizes = (B, Hq, T)
+    mask = (max_new, max_kv, int(r), int(W), int(sinks), int(window_mode))
+    need = unigist_paged_attn_workspace(C.byref(c), *sizes, *mask, int(weigh))
+    if need == 0:
+        raise UnigistError("unigist_paged_attn_workspace: invalid or unsupported arguments")
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    out = torch.empty_strided((Hq, T, D), (hs, rs, 1), dtype=q.dtype, device=q.device)
+    lse = torch.empty(Hq, T, dtype=torch.float32, device=q.device)
+    _check(unigist_paged_attn(C.byref(c), q.data_ptr(), out.data_ptr(), lse.data_ptr(), *sizes,
+                              None if cu is None else _int32(cu, B + 1, "cu"), _int32(kv_len, B, "kv_len"), *mask, hs, rs,
+                              int(weigh), float(decay), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                              _stream()),
+           "unigist_paged_attn")
+    return out, lse
+
+
+def paged_evict(k, v, table, kv_len, weight, keep, k_out, v_out, table_out, max_kv, max_keep, sinks=0, recent=0, weight_out=None):
+    """Keep, for every kv head of every sequence, keep[b] (int32 [B] on the GPU) of its rows: the first `sinks`, the last
+    `recent`, then those of most weight; they are copied in order to the rows 0, 1, .. under table_out in k_out, v_out (the
+    same pool or another; pages that table does not name) -> rows kept, int32 [B] (-1: a sequence left alone), and
+    their old row numbers, int32 [B, Hkv, max_keep] (-1 past the end)."""
+    c = _paged_cache(k, v, table, None, None, weight, values=False)
+    d = _paged_cache(k_out, v_out, table_out, None, None, weight_out, values=False)
+    B = table.shape[0]
+    if weight is None or table_out.shape[0] != B or (d.Hkv, d.D, d.dt) != (c.Hkv, c.D, c.dt):
+        raise UnigistError("paged_evict needs weights, and a destination of the same batch, heads, head dimension and dtype")
+    _same_device(k, v, table, kv_len, weight, keep, k_out, v_out, table_out, weight_out)
+    kept = torch.empty(B, c.Hkv, int(max_keep), dtype=torch.int32, device=k.device)
+    rows = torch.empty(B, dtype=torch.int32, device=k.device)
+    _check(unigist_paged_evict(C.byref(c), C.byref(d), B, _int32(kv_len, B, "kv_len"), _int32(keep, B, "keep"), int(max_kv),
+                               int(max_keep), int(sinks), int(recent), kept.data_ptr(), rows.data_ptr(), _stream()),
+           "unigist_paged_evict")
+    return rows, kept

@@ -1,0 +1,121 @@
+"""What the paged entry points refuse, before anything is launched (no GPU needed: no pointer is followed)."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2509_15763_amd as u
+
+FAKE = 0x1000
+OK, EINVAL, EUNSUPPORTED = 0, 1, 2
+
+
+def cache(**kw):
+    a = dict(k=FAKE, v=FAKE, k_scale=None, v_scale=None, weight=FAKE, table=FAKE, n_pages=10, page=16, table_cols=4, Hkv=2, D=64, dt=0)
+    a.update(kw)
+    return u.binding._PagedCache(*a.values())
+
+
+def attn(c=None, **kw):
+    a = dict(q=FAKE, out=FAKE, lse=FAKE, B=2, Hq=4, T=3, cu=FAKE, kv_len=FAKE, max_new=2, max_kv=64, r=4, W=8, sinks=0, mode=0, hs=64, rs=256, weigh=1,
+             decay=1.0, ws=FAKE, ws_bytes=1 << 40)
+    a.update(kw)
+    return u.unigist_paged_attn(C.byref(c or cache()), *a.values())
+
+
+def size(c=None, **kw):
+    a = dict(B=2, Hq=4, T=3, max_new=2, max_kv=64, r=4, W=8, sinks=0, mode=0, weigh=1)
+    a.update(kw)
+    return u.unigist_paged_attn_workspace(C.byref(c or cache()), *a.values())
+
+
+def append(c=None, **kw):
+    a = dict(k=FAKE, v=FAKE, hs=64, rs=128, B=2, T=3, cu=FAKE, kv_len=FAKE)
+    a.update(kw)
+    return u.unigist_paged_append(C.byref(c or cache()), *a.values())
+
+
+def evict(src=None, dst=None, **kw):
+    a = dict(B=2, kv_len=FAKE, keep=FAKE, max_kv=64, max_keep=32, sinks=0, recent=0, kept=FAKE, rows=FAKE)
+    a.update(kw)
+    return u.unigist_paged_evict(C.byref(src or cache()), C.byref(dst or cache()), *a.values())
+
+
+BAD_CACHES = [(dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(table=None), EINVAL), (dict(k=FAKE + 8), EINVAL), (dict(v=FAKE + 2), EINVAL), (dict(n_pages=0), EINVAL),
+              (dict(page=0), EINVAL), (dict(table_cols=0), EINVAL), (dict(Hkv=0), EINVAL), (dict(D=0), EINVAL), (dict(D=4), EUNSUPPORTED), (dict(D=100), EUNSUPPORTED),
+              (dict(D=136), EUNSUPPORTED), (dict(dt=1), EUNSUPPORTED), (dict(dt=7), EUNSUPPORTED), (dict(dt=2, D=72), EUNSUPPORTED),
+              (dict(n_pages=1 << 20, page=1 << 10), EUNSUPPORTED), (dict(n_pages=1 << 19, page=513), EUNSUPPORTED), (dict(n_pages=0x7FFFFFFF, page=0x7FFFFFFF, Hkv=0x7FFFFFFF), EUNSUPPORTED)]
+
+
+@pytest.mark.parametrize("kw,want", BAD_CACHES)
+def test_descriptors(kw, want):
+    c = cache(**kw)
+    assert attn(c) == want and size(c) == 0 and append(c) == want and evict(c) == want and evict(None, c) == want
+
+
+def test_codes_need_scales():
+    for kw in (dict(), dict(k_scale=FAKE), dict(v_scale=FAKE)):
+        c = cache(dt=2, **kw)
+        assert attn(c) == EINVAL and size(c) == 0 and append(c) == EINVAL
+
+
+@pytest.mark.parametrize("kw,want", [(dict(B=0), EINVAL), (dict(T=-1), EINVAL), (dict(Hq=3), EINVAL), (dict(Hq=0), EINVAL), (dict(max_new=0), EINVAL),
+                                     (dict(max_kv=0), EINVAL), (dict(r=0), EINVAL), (dict(W=0), EINVAL), (dict(sinks=-1), EINVAL), (dict(mode=2), EINVAL),
+                                     (dict(weigh=-1), EINVAL), (dict(B=1 << 20), EUNSUPPORTED), (dict(max_kv=(1 << 23) + 1), EUNSUPPORTED),
+                                     (dict(T=(1 << 23) + 1), EUNSUPPORTED)])
+def test_attn_sizes(kw, want):
+    assert attn(**kw) == want and size(**kw) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(q=None), dict(out=None), dict(lse=None), dict(cu=None), dict(kv_len=None), dict(q=FAKE + 2), dict(out=FAKE + 8), dict(hs=65), dict(rs=63),
+                                dict(rs=56), dict(hs=-64), dict(decay=-1.0), dict(decay=float("nan")), dict(decay=float("inf")), dict(ws=None), dict(ws=FAKE + 16),
+                                dict(ws_bytes=0)])
+def test_attn_arguments(kw):
+    assert attn(**kw) == EINVAL
+
+
+def test_weights_asked_for_and_not_there():
+    assert attn(cache(weight=None)) == EINVAL and size(cache(weight=None)) == 0
+    assert size(cache(weight=None), weigh=0) > 0
+
+
+def test_nothing_to_do():
+    # no new rows at all: fine, and nothing is launched
+    assert attn(T=0, q=None, out=None) == OK and append(T=0, k=None, v=None) == OK
+
+
+@pytest.mark.parametrize("kw,want", [(dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(kv_len=None), EINVAL), (dict(cu=None), EINVAL), (dict(k=FAKE + 2), EINVAL),
+                                     (dict(hs=4), EINVAL), (dict(rs=60), EINVAL), (dict(rs=1 << 31), EUNSUPPORTED), (dict(B=0), EINVAL), (dict(T=-1), EINVAL)])
+def test_append_arguments(kw, want):
+    assert append(**kw) == want
+
+
+@pytest.mark.parametrize("kw,want", [(dict(B=0), EINVAL), (dict(kv_len=None), EINVAL), (dict(keep=None), EINVAL), (dict(kept=None), EINVAL), (dict(rows=None), EINVAL),
+                                     (dict(max_kv=0), EINVAL), (dict(max_keep=0), EINVAL), (dict(sinks=-1), EINVAL), (dict(recent=-1), EINVAL),
+                                     (dict(max_kv=(1 << 23) + 1), EUNSUPPORTED), (dict(max_keep=(1 << 23) + 1), EUNSUPPORTED), (dict(B=1 << 17), EUNSUPPORTED)])
+def test_evict_arguments(kw, want):
+    assert evict(**kw) == want
+
+
+def test_evict_between_unlike_pools():
+    assert evict(cache(weight=None)) == EINVAL
+    for kw in (dict(Hkv=1), dict(D=128), dict(dt=2)):
+        assert evict(None, cache(**kw)) == EINVAL
+
+
+def test_the_workspace_does_not_depend_on_what_lies_in_device_memory():
+    assert size() == size(cache(k=FAKE + 4096, table=FAKE + 4))
+
+
+def test_bindings_refuse_tensors_that_are_not_on_the_gpu():
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    t, n = torch.zeros(1, 2, dtype=torch.int32), torch.ones(1, dtype=torch.int32)
+    q = torch.zeros(4, 1, 64, dtype=torch.bfloat16)
+    for call in (lambda: u.paged_attn(q, k, k, t, n, 4, 8), lambda: u.paged_append(k, k, t, n, q[:2], q[:2]),
+                 lambda: u.paged_evict(k, k, t, n, torch.zeros(4, 2, 16), n, k, k, t, 10, 5)):
+        with pytest.raises(u.UnigistError):
+            call()
+    with pytest.raises(u.UnigistError):
+        u.paged_attn(q, k.float(), k.float(), t, n, 4, 8)
+    with pytest.raises(u.UnigistError):
+        u.paged_attn(q, k.byte(), k.byte(), t, n, 4, 8)  # codes without scales
