@@ -17,7 +17,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libunigist.so")
 SOURCES = ["api.cpp", "blockmap.cpp", "attn_simple.hip", "attn_fwd_mfma.hip", "attn_bwd_mfma.hip", "decode.hip", "cache.hip", "probe.hip", "noalloc.hip",
-           "paged_api.cpp", "paged_attn.hip", "paged_cache.hip"]
+           "paged_api.cpp", "paged_attn.hip", "paged_decode.hip", "paged_chunk.hip", "paged_cache.hip"]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-x", "hip",

@@ -89,6 +89,61 @@ __host__ __device__ inline AttnShape mask_shape(const PagedMask& m) {
     return s;
 }
 
+// What a set of query rows at positions pf (the first, >= 0) to end - 1 walks: the `nfar` always-visible rows left of every
+// window, which all of them see, then the rows wstart .. end - 1, which each sees by the rule.  Numbered through as `E` entries.
+struct PagedWalk {
+    int wstart, nfar, E;
+};
+__host__ __device__ inline PagedWalk paged_walk(const AttnShape& m, int pf, int end) {
+    PagedWalk w;
+    w.wstart = win_lo(m, pf);
+    w.nfar = count_always(m, w.wstart);
+    w.E = w.nfar + (end - w.wstart);
+    return w;
+}
+__host__ __device__ inline int entry_row(const AttnShape& m, const PagedWalk& w, int e) {
+    return e < w.nfar ? pos_of_always(m, e) : e - w.nfar + w.wstart;
+}
+// A row of entry e as the kernels fetch it: byte offset / 16 from k or v (the host checks that it fits), or place 0 of the
+// pool with there = false where its page is not there.
+struct PagedPlace {
+    unsigned off;
+    bool there;
+};
+// first half: the table entry of a row (-1: the table has none), second half: the place.  Apart, so that the load can be in flight.
+__device__ __forceinline__ int page_id(const PagedKv& c, int b, int row) {
+    const int pg = page_of(c, row);
+    return pg < c.cols ? c.table[(size_t)b * c.cols + pg] : -1;
+}
+__device__ __forceinline__ PagedPlace place_of(const PagedKv& c, int hk, int row, int id, int row16) {
+    PagedPlace p;
+    p.there = (unsigned)id < (unsigned)c.n_pages;
+    const unsigned at = ((unsigned)id * c.Hkv + hk) * c.page + (row - page_of(c, row) * c.page);
+    p.off = p.there ? at * (unsigned)row16 : 0u;
+    return p;
+}
+
+// Entries of a walk are shared out in at most S slices of about `want` entries, all of one length (a multiple of `unit`).
+struct PagedSlices {
+    int n, per;
+};
+__host__ __device__ inline PagedSlices paged_slices(int E, int S, int want, int unit) {
+    PagedSlices x;
+    x.n = (E + want - 1) / want;
+    x.n = x.n > S ? S : x.n < 1 ? 1 : x.n;
+    x.per = ((E + x.n - 1) / x.n + unit - 1) / unit * unit;
+    x.n = x.per > 0 ? (E + x.per - 1) / x.per : 1;  // rounding up may leave fewer
+    if (x.n < 1) x.n = 1;
+    return x;
+}
+// Partial results of slices: per (unit, slice, column) the running reference m (exponent of 2) and sum l, and the
+// accumulator of built-for width.
+struct PagedParts {
+    float* ml;   // [units][S][cols][2]
+    float* acc;  // [units][S][cols][D]
+    int S, want, cols;
+};
+
 struct PagedAttn {
     PagedKv kv;
     PagedBatch batch;

@@ -1,104 +1,284 @@
-// Attention of the new rows of a batch over a paged cache, and the attention weight that the cached rows receive.
-#include "paged.h"
+// Attention over a paged cache: the choice of kernels, the merge of slices, and the weight that the cached rows receive.
+#include <algorithm>
+
+#include "paged_common.h"
 
 namespace unigist {
+
+hipError_t launch_paged_decode(const PagedAttn& a, bool e4m3, const PagedParts& parts, int cols, hipStream_t st);
+hipError_t launch_paged_chunk(const PagedAttn& a, bool e4m3, const PagedParts& parts, int ntiles, int min_cols, hipStream_t st);
+
 namespace {
 
-__device__ __forceinline__ void load8(const PagedKv& c, const char* pool, bool e4m3, int at, int d, float (&x)[8]) {
-    if (e4m3) {
-        const u32x2 w = *(const u32x2*)(pool + (size_t)at * c.D + d);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-            x[4 * i] = lo[0], x[4 * i + 1] = lo[1], x[4 * i + 2] = hi[0], x[4 * i + 3] = hi[1];
+// ---------------------------------------------------------------------------------------------
+// Merge of the slices of a column.  W waves a column, each taking every W-th slice; all loads of up to kBatch slices are
+// in flight.  CHUNK: units are tiles of the chunk kernel, else (sequence, kv head) pairs of the decode kernel.
+constexpr int kBatch = 8;
+template <int D, int W, bool CHUNK>
+__global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a, PagedParts parts, int limit) {
+    constexpr int C = (D + 63) / 64;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int part = wave % W, col = blockIdx.x * (4 / W) + wave / W, hk = blockIdx.y;
+    const int Hkv = a.kv.Hkv, G = a.Hq / Hkv;
+    __shared__ float sums[4][64 * C];
+    int b = CHUNK ? 0 : blockIdx.z, c0 = 0;
+    if (CHUNK) {
+        const int tile = blockIdx.z;
+        int hi = a.batch.B - 1;
+        while (b < hi) {
+            const int mid = (b + hi + 1) >> 1;
+            const int first = (int)((unsigned)((a.batch.cu ? min(max(a.batch.cu[mid], 0), a.batch.T) : mid) * G) / kChunkCols) + mid;
+            if (first <= tile) b = mid;
+            else hi = mid - 1;
         }
+    }
+    const PagedSeq s = paged_seq(a.batch, b);
+    const int ncol = s.n * G;
+    int last = s.len - 1, first = s.p0;  // positions that the slices were made of
+    bool mine;
+    if (CHUNK) {
+        c0 = ((int)blockIdx.z - ((int)((unsigned)(s.t0 * G) / kChunkCols) + b)) * kChunkCols;
+        mine = ncol > limit && c0 >= 0 && c0 < ncol && c0 + col < ncol;
+        const int c1 = min(c0 + kChunkCols, ncol) - 1;
+        first = s.p0 + c0 / G;
+        last = s.p0 + c1 / G;
     } else {
-        const u32x4 w = *(const u32x4*)(pool + ((size_t)at * c.D + d) * 2);
+        mine = ncol > 0 && ncol <= limit && col < ncol;
+    }
+    const AttnShape m = mask_shape(a.mask);
+    const int E = last >= 0 && mine ? paged_walk(m, max(first, 0), last + 1).E : 0;
+    const int n = paged_slices(E, parts.S, parts.want, CHUNK ? 32 : 128).n;
+    mine = mine && n > 1;
+    float acc[C], mm = -INFINITY, ll = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-
-// One wave per query row and head: 16 lanes a key, four keys at a time, running maximum and sum.
-__global__ __launch_bounds__(64) void paged_attn_simple_kernel(PagedAttn a, bool e4m3) {
-    const int t = blockIdx.x, hq = blockIdx.y, lane = threadIdx.x, sub = lane & 15, grp = lane >> 4;
-    const int b = seq_of_row(a.batch, t), hk = hq / (a.Hq / a.kv.Hkv);
-    const PagedSeq s = paged_seq(a.batch, b);
-    if (t < s.t0 || t >= s.t0 + s.n) return;
-    const AttnShape m = mask_shape(a.mask);
-    const int p = s.p0 + (t - s.t0), d = 8 * sub;
-    const bool have = d < a.kv.D;
-    const float sc = a.scale * (a.kv.kscale ? a.kv.kscale[hk] : 1.f);
-    float q[8] = {}, acc[8] = {}, mx = -INFINITY, l = 0.f;
-    const size_t at_q = (size_t)hq * a.q_hs + (size_t)t * a.q_rs + d;
-    if (have)
-        for (int i = 0; i < 8; ++i) q[i] = bf16_to_f32(a.q[at_q + i]) * sc;
-    for (int j = grp; j <= p; j += 4) {
-        if (!is_always(m, j) && j < win_lo(m, p)) continue;
-        const int at = pool_row(a.kv, b, hk, j);
-        if (at < 0) continue;
-        float k[8] = {}, v[8] = {}, x = 0.f;
-        if (have) {
-            load8(a.kv, a.kv.k, e4m3, at, d, k);
-            load8(a.kv, a.kv.v, e4m3, at, d, v);
-        }
-        for (int i = 0; i < 8; ++i) x = fmaf(q[i], k[i], x);
-        for (int off = 1; off < 16; off <<= 1) x += __shfl_xor(x, off, 16);
-        const float mn = fmaxf(mx, x), old = mx == -INFINITY ? 0.f : __expf(mx - mn), w = mn == -INFINITY ? 0.f : __expf(x - mn);
-        l = l * old + w;
-        for (int i = 0; i < 8; ++i) acc[i] = acc[i] * old + w * v[i];
-        mx = mn;
-    }
-    for (int off = 16; off < 64; off <<= 1) {
-        const float om = __shfl_xor(mx, off, 64), mn = fmaxf(mx, om);
-        const float f = mx == -INFINITY ? 0.f : __expf(mx - mn), g = om == -INFINITY ? 0.f : __expf(om - mn);
-        l = l * f + __shfl_xor(l, off, 64) * g;
-        for (int i = 0; i < 8; ++i) acc[i] = acc[i] * f + __shfl_xor(acc[i], off, 64) * g;
-        mx = mn;
-    }
-    const float inv = (a.kv.vscale ? a.kv.vscale[hk] : 1.f) / l;
-    if (grp == 0 && have)
-        for (int i = 0; i < 8; ++i) a.out[at_q + i] = f32_to_bf16(mx == -INFINITY ? 0.f : acc[i] * inv);
-    if (a.lse && lane == 0) a.lse[(size_t)hq * a.batch.T + t] = mx == -INFINITY ? -INFINITY : mx + __logf(l);
-}
-
-// One lane per cached row: the sum over the last new rows and the heads of the group of exp(score - lse).
-__global__ __launch_bounds__(64) void paged_weigh_simple_kernel(PagedAttn a, bool e4m3) {
-    const int b = blockIdx.z, hk = blockIdx.y, j = blockIdx.x * 64 + threadIdx.x, G = a.Hq / a.kv.Hkv;
-    const PagedSeq s = paged_seq(a.batch, b);
-    if (j >= s.len || s.n == 0) return;
-    const int at = pool_row(a.kv, b, hk, j);
-    if (at < 0) return;
-    const AttnShape m = mask_shape(a.mask);
-    const float sc = a.scale * (a.kv.kscale ? a.kv.kscale[hk] : 1.f);
-    float sum = 0.f;
-    for (int i = max(0, s.n - a.weigh); i < s.n; ++i) {
-        const int p = s.p0 + i;
-        if (j > p || (!is_always(m, j) && j < win_lo(m, p))) continue;
-        for (int g = 0; g < G; ++g) {
-            const int hq = hk * G + g, t = s.t0 + i;
-            const bf16_t* q = a.q + (size_t)hq * a.q_hs + (size_t)t * a.q_rs;
-            float x = 0.f;
-            for (int d = 0; d < a.kv.D; d += 8) {
-                float k[8];
-                load8(a.kv, a.kv.k, e4m3, at, d, k);
-                for (int e = 0; e < 8; ++e) x = fmaf(bf16_to_f32(q[d + e]), k[e], x);
+    for (int i = 0; i < C; ++i) acc[i] = 0.f;
+    if (mine) {
+        const size_t unit = CHUNK ? (size_t)blockIdx.z * Hkv + hk : (size_t)b * Hkv + hk;
+        const size_t stride = parts.cols;  // columns between slices
+        const size_t at0 = unit * parts.S * stride + col;
+        float x[kBatch][C];
+        auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+                for (int k = 0; k < C; ++k) x[i][k] = parts.acc[(at0 + min(s0 + W * i, n - 1) * stride) * D + min(64 * k + lane, D - 1)];
+        };
+        load(part);
+        const f32x2 ml = lane < n ? *(const f32x2*)(parts.ml + 2 * (at0 + lane * stride)) : f32x2{-INFINITY, 0.f};  // n <= 64
+        mm = ml[0];
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) mm = fmaxf(mm, __shfl_xor(mm, off, 64));
+        // a slice in which the column sees nothing has l = 0; one with scores that are no numbers l = NaN and any m
+        const float wgt = ml[1] == 0.f ? 0.f : ml[0] == mm ? 1.f : __builtin_amdgcn_exp2f(ml[0] - mm);
+        const unsigned long long has = __builtin_amdgcn_ballot_w64(!(ml[1] == 0.f));
+        ll = wgt * ml[1];
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) ll += __shfl_xor(ll, off, 64);
+        for (int s0 = part; s0 < n; s0 += W * kBatch) {
+            if (s0 != part) load(s0);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int t = s0 + W * i;
+                const float f = __shfl(wgt, t < n ? t : 0, 64);
+                if (t < n && (has >> t & 1))
+#pragma unroll
+                    for (int k = 0; k < C; ++k) acc[k] += f * x[i][k];
             }
-            const float lse = a.lse[(size_t)hq * a.batch.T + t];
-            if (lse != -INFINITY) sum += __expf(x * sc - lse);
         }
     }
-    a.kv.weight[at] = a.decay == 0.f ? sum : a.decay * a.kv.weight[at] + sum;
+    if (W > 1) {
+#pragma unroll
+        for (int k = 0; k < C; ++k) sums[wave][64 * k + lane] = acc[k];
+        __syncthreads();
+        if (part != 0) return;
+#pragma unroll
+        for (int k = 0; k < C; ++k) acc[k] = (sums[wave][64 * k + lane] + sums[wave + 1][64 * k + lane]) + (sums[wave + 2][64 * k + lane] + sums[wave + 3][64 * k + lane]);
+    }
+    if (!mine) return;
+    const int i = (c0 + col) / G, hq = hk * G + (c0 + col - i * G), t = s.t0 + i;
+#pragma unroll
+    for (int k = 0; k < C; ++k)
+        if (64 * k + lane < a.kv.D)
+            Elem<bf16_t>::store(a.out + (size_t)hq * a.q_hs + (size_t)t * a.q_rs + 64 * k + lane, ll == 0.f ? 0.f : acc[k] / ll);
+    if (lane == 0 && a.lse) a.lse[(size_t)hq * a.batch.T + t] = ll == 0.f ? -INFINITY : mm * kLn2 + __builtin_amdgcn_logf(ll) * kLn2;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Weights: the scores of the last new rows once more, summed over columns instead of keys.  A wave holds 32 keys of one kv
+// head (A operand K, in registers) and walks the columns 16 at a time (B operand Q^T); exp(score - lse) of the visible pairs
+// adds up per lane, over its 16 columns at the end.
+template <int D, bool E4M3>
+__global__ __launch_bounds__(256) void paged_weigh_kernel(PagedAttn a) {
+    constexpr int KS = D / 32;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r16 = lane & 15, g4 = lane >> 4;
+    const int hk = blockIdx.y, b = blockIdx.z, j0 = blockIdx.x * 128 + 32 * w;
+    const int G = a.Hq / a.kv.Hkv, Dt = a.kv.D;
+    const PagedSeq s = paged_seq(a.batch, b);
+    if (j0 >= s.len || s.n == 0) return;
+    const AttnShape m = mask_shape(a.mask);
+    const float c = a.scale * (E4M3 ? a.kv.kscale[hk] : 1.f) * kLog2e;
+    bf16x8 kf[2][KS];
+    const int row_bytes = Dt * (E4M3 ? 1 : 2), row16 = row_bytes / 16;
+    PagedPlace mine;
+    {
+        const int j = min(j0 + (lane & 31), s.len - 1);
+        mine = place_of(a.kv, hk, j, page_id(a.kv, b, j), row16);
+    }
+    const unsigned gone = (unsigned)__builtin_amdgcn_ballot_w64(!mine.there || j0 + (lane & 31) >= s.len);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+        const char* p = a.kv.k + ((size_t)(unsigned)__shfl((int)mine.off, 16 * kb + r16, 64) << 4);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int e = 32 * ks + 8 * g4;
+            u32x4 x = {0u, 0u, 0u, 0u};
+            if (e < Dt) {
+                if constexpr (E4M3) {
+                    const u32x2 y = *(const u32x2*)(p + e);
+                    const u32x2 p0 = widen4(y[0]), p1 = widen4(y[1]);
+                    x = u32x4{p0[0], p0[1], p1[0], p1[1]};
+                } else {
+                    x = *(const u32x4*)(p + 2 * e);
+                }
+            }
+            kf[kb][ks] = __builtin_bit_cast(bf16x8, x);
+        }
+    }
+    float sum[2][4] = {};
+    const int i0 = max(max(0, s.n - a.weigh), j0 - s.p0);  // rows before j0's position see none of these keys
+    const int ncol = s.n * G;
+    for (int c0 = i0 * G; c0 < ncol; c0 += 16) {
+        const int col = min(c0 + r16, ncol - 1), i = col / G, h = col - i * G, t = s.t0 + i, p = s.p0 + i;
+        const bf16_t* q = a.q + (size_t)(hk * G + h) * a.q_hs + (size_t)t * a.q_rs;
+        bf16x8 qf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            u32x4 z = {0u, 0u, 0u, 0u};
+            if (32 * ks + 8 * g4 < Dt) z = *(const u32x4*)(q + 32 * ks + 8 * g4);
+            qf[ks] = __builtin_bit_cast(bf16x8, z);
+        }
+        const float lse = a.lse[(size_t)(hk * G + h) * a.batch.T + t];
+        unsigned vis = 0u;
+        {
+            const int lo = p >= 0 ? win_lo(m, p) : 0;
+            unsigned gists = 0u;
+            if (__builtin_amdgcn_ballot_w64(j0 < lo) != 0ull) gists = (unsigned)__builtin_amdgcn_ballot_w64(lane < 32 && is_always(m, j0 + lane));
+            if (p >= 0 && c0 + r16 < ncol && lse != -INFINITY) vis = (bits_below(p - j0 + 1) & (~bits_below(lo - j0) | gists) & ~gone) >> (4 * g4);
+        }
+        f32x4 sa[2] = {zero4(), zero4()};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            sa[0] = mfma16(kf[0][ks], qf[ks], sa[0]);
+            sa[1] = mfma16(kf[1][ks], qf[ks], sa[1]);
+        }
+        const float l2 = lse * kLog2e;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i2 = 0; i2 < 4; ++i2) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(sa[kb][i2], c, -l2));
+                sum[kb][i2] += (vis >> (16 * kb + i2)) & 1u ? x : 0.f;
+            }
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int off = 1; off < 16; off <<= 1) sum[kb][i] += __shfl_xor(sum[kb][i], off, 64);
+            const int j = j0 + 16 * kb + 4 * g4 + i;
+            const int at = r16 == 4 * kb + i && j < s.len ? pool_row(a.kv, b, hk, j) : -1;
+            if (at >= 0) a.kv.weight[at] = a.decay == 0.f ? sum[kb][i] : fmaf(a.decay, a.kv.weight[at], sum[kb][i]);
+        }
+}
+
+// ---------------------------------------------------------------------------------------------
+// The launch: sequences of few columns (new rows x heads of a group) go to the decode kernel, the others to the chunk
+// kernel; a batch that may hold both launches both, and each leaves the other's sequences.
+struct Plan {
+    int few;      // columns that the decode kernel takes at most (0: not launched)
+    bool chunk;   // is the chunk kernel launched?
+    int ntiles;
+    PagedParts dec, chk;
+    size_t bytes;
+};
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+int built_for(int D) { return D <= 64 ? 64 : D <= 96 ? 96 : 128; }
+
+Plan make_plan(const PagedAttn& a, char* ws) {
+    Plan p = {};
+    const int G = a.Hq / a.kv.Hkv, Hkv = a.kv.Hkv, B = a.batch.B, T = a.batch.T, D = built_for(a.kv.D);
+    const AttnShape m = mask_shape(a.mask);
+    const long most = (long)a.batch.max_new * G;  // columns of a sequence at most
+    p.few = most <= 16 ? 16 : 32;
+    p.chunk = most > p.few;
+    if (B == 1 && p.chunk) p.few = 0;
+    size_t off = 0;
+    auto place = [&](PagedParts& x, size_t units, int cols) {
+        x.cols = cols;
+        if (x.S <= 1) return;
+        const size_t n = units * x.S * cols;
+        x.ml = (float*)(ws + off);
+        off += align256(n * 2 * sizeof(float));
+        x.acc = (float*)(ws + off);
+        off += align256(n * D * sizeof(float));
+    };
+    if (p.few) {
+        const int E = paged_walk(m, a.batch.max_kv - 1, a.batch.max_kv).E;
+        const long units = (long)B * Hkv;
+        int want = (int)std::min<long>((long)E * units / 1024 + 1, 1 << 24);
+        want = std::max(want, units <= 64 ? 128 : 256);
+        want = std::max(want, (E + 63) / 64);
+        p.dec.want = (want + 127) / 128 * 128;
+        p.dec.S = std::min(64, std::max(1, (E + p.dec.want - 1) / p.dec.want));
+        place(p.dec, (size_t)B * Hkv, (int)std::min<long>(p.few, most));
+    }
+    if (p.chunk) {
+        p.ntiles = (int)((long)T * G / kChunkCols) + B;
+        const long units = (long)p.ntiles * Hkv;
+        const int rows = std::min(a.batch.max_new, kChunkCols / G + 1);
+        const int E = paged_walk(m, std::max(0, a.batch.max_kv - rows), a.batch.max_kv).E;
+        int S = units >= 512 ? 1 : (int)std::min<long>(32, (768 + units - 1) / units);
+        S = std::max(1, std::min(S, (E + 255) / 256));
+        p.chk.S = S;
+        p.chk.want = S == 1 ? 1 << 24 : std::max(256, (E + S - 1) / S);
+        place(p.chk, (size_t)units, kChunkCols);
+    }
+    p.bytes = std::max<size_t>(off, 256);
+    return p;
+}
+
+template <int D>
+hipError_t launch_combine(const PagedAttn& a, const Plan& p, hipStream_t st) {
+    if (p.few && p.dec.S > 1) {
+        const int cols = p.dec.cols;
+        if (p.dec.S > 8) paged_combine_kernel<D, 4, false><<<dim3(cols, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, p.dec, cols);
+        else paged_combine_kernel<D, 1, false><<<dim3((cols + 3) / 4, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, p.dec, cols);
+    }
+    if (p.chunk && p.chk.S > 1)
+        paged_combine_kernel<D, 1, true><<<dim3(kChunkCols / 4, a.kv.Hkv, p.ntiles), 256, 0, st>>>(a, p.chk, p.few);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t paged_attn_bytes(const PagedAttn& a, bool e4m3) { return 256; }
+size_t paged_attn_bytes(const PagedAttn& a, bool) { return make_plan(a, nullptr).bytes; }
 
 hipError_t launch_paged_attn(const PagedAttn& a, bool e4m3, void* ws, hipStream_t st) {
-    paged_attn_simple_kernel<<<dim3(a.batch.T, a.Hq), 64, 0, st>>>(a, e4m3);
-    if (a.weigh)
-        paged_weigh_simple_kernel<<<dim3((a.batch.max_kv + 63) / 64, a.kv.Hkv, a.batch.B), 64, 0, st>>>(a, e4m3);
+    const Plan p = make_plan(a, (char*)ws);
+    hipError_t e = hipSuccess;
+    if (p.chunk) e = launch_paged_chunk(a, e4m3, p.chk, p.ntiles, p.few, st);
+    if (e == hipSuccess && p.few) e = launch_paged_decode(a, e4m3, p.dec, p.few, st);
+    const int D = built_for(a.kv.D);
+    if (e == hipSuccess) e = D == 64 ? launch_combine<64>(a, p, st) : D == 96 ? launch_combine<96>(a, p, st) : launch_combine<128>(a, p, st);
+    if (e != hipSuccess || !a.weigh) return e;
+    const dim3 grid((a.batch.max_kv + 127) / 128, a.kv.Hkv, a.batch.B);
+    auto go = [&](auto kern) { kern<<<grid, 256, 0, st>>>(a); };
+    if (D == 64) e4m3 ? go(paged_weigh_kernel<64, true>) : go(paged_weigh_kernel<64, false>);
+    else if (D == 96) e4m3 ? go(paged_weigh_kernel<96, true>) : go(paged_weigh_kernel<96, false>);
+    else e4m3 ? go(paged_weigh_kernel<128, true>) : go(paged_weigh_kernel<128, false>);
     return hipGetLastError();
 }
 
