@@ -144,6 +144,13 @@ struct PagedParts {
     int S, want, cols;
 };
 
+// Scores of few columns in exponents of 2, -inf where a column does not see the entry: [B * Hkv][cols][pitch], pitch >= entries.
+struct PagedScores {
+    float* x;
+    int cols;
+    int pitch;
+};
+
 struct PagedAttn {
     PagedKv kv;
     PagedBatch batch;

@@ -5,7 +5,7 @@
 
 namespace unigist {
 
-hipError_t launch_paged_decode(const PagedAttn& a, bool e4m3, const PagedParts& parts, int cols, hipStream_t st);
+hipError_t launch_paged_decode(const PagedAttn& a, bool e4m3, const PagedParts& parts, const PagedScores& scores, int cols, hipStream_t st);
 hipError_t launch_paged_chunk(const PagedAttn& a, bool e4m3, const PagedParts& parts, int ntiles, int min_cols, hipStream_t st);
 
 namespace {
@@ -104,102 +104,178 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a, PagedPa
 }
 
 // ---------------------------------------------------------------------------------------------
-// Weights: the scores of the last new rows once more, summed over columns instead of keys.  A wave holds 32 keys of one kv
-// head (A operand K, in registers) and walks the columns 16 at a time (B operand Q^T); exp(score - lse) of the visible pairs
-// adds up per lane, over its 16 columns at the end.
+// Weights of a sequence of many columns: the scores of the last new rows once more, summed over columns instead of keys.  A
+// wave holds 64 keys of one kv head (A operand K, in registers); the columns come in chunks of 64 through two LDS stages
+// (B operand Q^T, direct loads, chunks swizzled as in the attention kernels) with their position, the start of their window
+// and their lse, and exp(score - lse) of the visible pairs adds up per lane, over a lane's 16 columns at the end.
+// Bound by the matrix pipe and the exponentials, K is read once.
+constexpr int kWeighKeys = 256, kWeighCols = 64;
 template <int D, bool E4M3>
-__global__ __launch_bounds__(256) void paged_weigh_kernel(PagedAttn a) {
-    constexpr int KS = D / 32;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r16 = lane & 15, g4 = lane >> 4;
-    const int hk = blockIdx.y, b = blockIdx.z, j0 = blockIdx.x * 128 + 32 * w;
+__global__ __launch_bounds__(256, 2) void paged_weigh_kernel(PagedAttn a, int min_cols) {
+    constexpr int KS = D / 32, CH = D <= 64 ? 8 : 16, RPI = 64 / CH, IPW = 16 / RPI;
+    __shared__ __attribute__((aligned(1024))) char qs[2][kWeighCols * CH * 16];
+    __shared__ float ls[2][kWeighCols];
+    __shared__ int ps[2][kWeighCols], los[2][kWeighCols];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g4 = lane >> 4;
+    const int hk = blockIdx.y, b = blockIdx.z, wg0 = blockIdx.x * kWeighKeys, j0 = wg0 + 64 * w;
     const int G = a.Hq / a.kv.Hkv, Dt = a.kv.D;
     const PagedSeq s = paged_seq(a.batch, b);
-    if (j0 >= s.len || s.n == 0) return;
+    const int ncol = s.n * G;
+    if (wg0 >= s.len || ncol <= min_cols) return;
     const AttnShape m = mask_shape(a.mask);
     const float c = a.scale * (E4M3 ? a.kv.kscale[hk] : 1.f) * kLog2e;
-    bf16x8 kf[2][KS];
+
+    // ---- this wave's keys
+    bf16x8 kf[4][KS];
     const int row_bytes = Dt * (E4M3 ? 1 : 2), row16 = row_bytes / 16;
-    PagedPlace mine;
+    unsigned long long gone;
     {
-        const int j = min(j0 + (lane & 31), s.len - 1);
-        mine = place_of(a.kv, hk, j, page_id(a.kv, b, j), row16);
+        const int j = min(j0 + lane, s.len - 1);
+        const PagedPlace mine = place_of(a.kv, hk, j, page_id(a.kv, b, j), row16);
+        gone = __builtin_amdgcn_ballot_w64(!mine.there || j0 + lane >= s.len);
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const char* p = a.kv.k + ((size_t)(unsigned)__shfl((int)mine.off, 16 * kb + r16, 64) << 4);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int e = 32 * ks + 8 * g4;
+                u32x4 x = {0u, 0u, 0u, 0u};
+                if (e < Dt) {
+                    if constexpr (E4M3) {
+                        const u32x2 y = *(const u32x2*)(p + e);
+                        const u32x2 p0 = widen4(y[0]), p1 = widen4(y[1]);
+                        x = u32x4{p0[0], p0[1], p1[0], p1[1]};
+                    } else {
+                        x = *(const u32x4*)(p + 2 * e);
+                    }
+                }
+                kf[kb][ks] = __builtin_bit_cast(bf16x8, x);
+            }
+        }
     }
-    const unsigned gone = (unsigned)__builtin_amdgcn_ballot_w64(!mine.there || j0 + (lane & 31) >= s.len);
+    float sum[4][4] = {};
+
+    // ---- columns, from the first new row that counts and sees any of these keys
+    const int i0 = max(max(0, s.n - a.weigh), wg0 - s.p0);
+    const int c0 = i0 * G, nchunks = (ncol - c0 + kWeighCols - 1) / kWeighCols;
+    auto issue = [&](int ch, int buf) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-        const char* p = a.kv.k + ((size_t)(unsigned)__shfl((int)mine.off, 16 * kb + r16, 64) << 4);
+        for (int i = 0; i < IPW; ++i) {
+            const int row = (w * IPW + i) * RPI + lane / CH, col = min(c0 + ch * kWeighCols + row, ncol - 1);
+            const int n = col / G, h = col - n * G, sc = (lane % CH) ^ swz16<CH>(row);
+            const bf16_t* q = a.q + (size_t)(hk * G + h) * a.q_hs + (size_t)(s.t0 + n) * a.q_rs + (8 * sc < Dt ? 8 * sc : 0);
+            g2l16(q, &qs[buf][(w * IPW + i) * 1024]);
+        }
+        if (tid < kWeighCols) {
+            const int col = min(c0 + ch * kWeighCols + tid, ncol - 1), n = col / G, h = col - n * G, p = s.p0 + n;
+            const float x = a.lse[(size_t)(hk * G + h) * a.batch.T + s.t0 + n];
+            // a column past the end, or one that sees nothing, sees no key here
+            const bool none = c0 + ch * kWeighCols + tid >= ncol || x == -INFINITY;
+            ls[buf][tid] = none ? 0.f : x * kLog2e;
+            ps[buf][tid] = none ? -1 : p;
+            los[buf][tid] = none || p < 0 ? 0x7fffffff : win_lo(m, p);
+        }
+    };
+    if (nchunks > 0) issue(0, 0);
+    for (int ch = 0; ch < nchunks; ++ch) {
+        const int buf = ch & 1;
+        wait_vmem();
+        __syncthreads();
+        if (ch + 1 < nchunks) issue(ch + 1, buf ^ 1);
+        if (j0 >= s.len) continue;  // a wave without keys only stages
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const int e = 32 * ks + 8 * g4;
-            u32x4 x = {0u, 0u, 0u, 0u};
-            if (e < Dt) {
-                if constexpr (E4M3) {
-                    const u32x2 y = *(const u32x2*)(p + e);
-                    const u32x2 p0 = widen4(y[0]), p1 = widen4(y[1]);
-                    x = u32x4{p0[0], p0[1], p1[0], p1[1]};
-                } else {
-                    x = *(const u32x4*)(p + 2 * e);
+        for (int cb = 0; cb < kWeighCols / 16; ++cb) {
+            const int p = ps[buf][16 * cb + r16], lo = los[buf][16 * cb + r16];
+            const float l2 = ls[buf][16 * cb + r16];
+            if (__builtin_amdgcn_ballot_w64(p >= j0) == 0ull) continue;
+            bf16x8 qf[KS];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                u32x4 x = *(const u32x4*)(qs[buf] + 16 * cb * CH * 16 + row16_lane_off<CH>(ks));
+                if (D > Dt && 32 * ks + 8 * g4 >= Dt) x = u32x4{0u, 0u, 0u, 0u};
+                qf[ks] = __builtin_bit_cast(bf16x8, x);
+            }
+            f32x4 sa[4];
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                sa[kb] = zero4();
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) sa[kb] = mfma16(kf[kb][ks], qf[ks], sa[kb]);
+            }
+            if (gone != 0ull || __builtin_amdgcn_ballot_w64(p < j0 + 63 || lo > j0) != 0ull) {
+                unsigned gists[2] = {0u, 0u};
+                if (__builtin_amdgcn_ballot_w64(p >= 0 && lo > j0) != 0ull) {
+                    const unsigned long long g = __builtin_amdgcn_ballot_w64(is_always(m, j0 + lane));
+                    gists[0] = (unsigned)g;
+                    gists[1] = (unsigned)(g >> 32);
+                }
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb) {
+                    const int j = j0 + 32 * (kb / 2);
+                    const unsigned vis = p < 0 ? 0u : (bits_below(p - j + 1) & (~bits_below(lo - j) | gists[kb / 2]) & ~(unsigned)(gone >> (32 * (kb / 2))));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!((vis >> (16 * (kb % 2) + 4 * g4 + i)) & 1u)) sa[kb][i] = -INFINITY;
                 }
             }
-            kf[kb][ks] = __builtin_bit_cast(bf16x8, x);
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[kb][i] += __builtin_amdgcn_exp2f(fmaf(sa[kb][i], c, -l2));
         }
     }
-    float sum[2][4] = {};
-    const int i0 = max(max(0, s.n - a.weigh), j0 - s.p0);  // rows before j0's position see none of these keys
-    const int ncol = s.n * G;
-    for (int c0 = i0 * G; c0 < ncol; c0 += 16) {
-        const int col = min(c0 + r16, ncol - 1), i = col / G, h = col - i * G, t = s.t0 + i, p = s.p0 + i;
-        const bf16_t* q = a.q + (size_t)(hk * G + h) * a.q_hs + (size_t)t * a.q_rs;
-        bf16x8 qf[KS];
+    if (j0 >= s.len) return;
+    float own = 0.f;  // lane r16 ends with the key 16 (r16 / 4) + 4 g4 + r16 % 4
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            u32x4 z = {0u, 0u, 0u, 0u};
-            if (32 * ks + 8 * g4 < Dt) z = *(const u32x4*)(q + 32 * ks + 8 * g4);
-            qf[ks] = __builtin_bit_cast(bf16x8, z);
-        }
-        const float lse = a.lse[(size_t)(hk * G + h) * a.batch.T + t];
-        unsigned vis = 0u;
-        {
-            const int lo = p >= 0 ? win_lo(m, p) : 0;
-            unsigned gists = 0u;
-            if (__builtin_amdgcn_ballot_w64(j0 < lo) != 0ull) gists = (unsigned)__builtin_amdgcn_ballot_w64(lane < 32 && is_always(m, j0 + lane));
-            if (p >= 0 && c0 + r16 < ncol && lse != -INFINITY) vis = (bits_below(p - j0 + 1) & (~bits_below(lo - j0) | gists) & ~gone) >> (4 * g4);
-        }
-        f32x4 sa[2] = {zero4(), zero4()};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            sa[0] = mfma16(kf[0][ks], qf[ks], sa[0]);
-            sa[1] = mfma16(kf[1][ks], qf[ks], sa[1]);
-        }
-        const float l2 = lse * kLog2e;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int i2 = 0; i2 < 4; ++i2) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(sa[kb][i2], c, -l2));
-                sum[kb][i2] += (vis >> (16 * kb + i2)) & 1u ? x : 0.f;
-            }
-    }
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
             for (int off = 1; off < 16; off <<= 1) sum[kb][i] += __shfl_xor(sum[kb][i], off, 64);
-            const int j = j0 + 16 * kb + 4 * g4 + i;
-            const int at = r16 == 4 * kb + i && j < s.len ? pool_row(a.kv, b, hk, j) : -1;
-            if (at >= 0) a.kv.weight[at] = a.decay == 0.f ? sum[kb][i] : fmaf(a.decay, a.kv.weight[at], sum[kb][i]);
+            if (r16 == 4 * kb + i) own = sum[kb][i];
         }
+    const int j = j0 + 16 * (r16 >> 2) + 4 * g4 + (r16 & 3);
+    const int at = j < s.len ? pool_row(a.kv, b, hk, j) : -1;
+    if (at >= 0) a.kv.weight[at] = a.decay == 0.f ? own : fmaf(a.decay, a.kv.weight[at], own);
+}
+
+// Weights of a sequence of few columns, from the scores that the decode kernel has left: one lane per row.
+__global__ __launch_bounds__(256) void paged_weigh_few_kernel(PagedAttn a, PagedScores scores) {
+    const int hk = blockIdx.y, b = blockIdx.z, j = blockIdx.x * 256 + threadIdx.x;
+    const int G = a.Hq / a.kv.Hkv;
+    const PagedSeq s = paged_seq(a.batch, b);
+    const int ncol = s.n * G;
+    if (ncol == 0 || ncol > scores.cols || j >= s.len) return;
+    const int at = pool_row(a.kv, b, hk, j);
+    if (at < 0) return;
+    const AttnShape m = mask_shape(a.mask);
+    const PagedWalk walk = paged_walk(m, max(s.p0, 0), s.len);
+    const int e = j >= walk.wstart ? walk.nfar + j - walk.wstart : is_always(m, j) ? count_always(m, j) : -1;
+    float sum = 0.f;
+    if (e >= 0) {
+        const float* x = scores.x + ((size_t)b * a.kv.Hkv + hk) * scores.cols * scores.pitch + e;
+        for (int i = max(0, s.n - a.weigh); i < s.n; ++i)
+            for (int g = 0; g < G; ++g) {
+                const float lse = a.lse[(size_t)(hk * G + g) * a.batch.T + s.t0 + i];
+                if (lse != -INFINITY) sum += __builtin_amdgcn_exp2f(fmaf(-lse, kLog2e, x[(size_t)(i * G + g) * scores.pitch]));
+            }
+    }
+    a.kv.weight[at] = a.decay == 0.f ? sum : fmaf(a.decay, a.kv.weight[at], sum);
 }
 
 // ---------------------------------------------------------------------------------------------
 // The launch: sequences of few columns (new rows x heads of a group) go to the decode kernel, the others to the chunk
 // kernel; a batch that may hold both launches both, and each leaves the other's sequences.
+// Scores of few columns are kept for the weights, 4 bytes a column and key for the 128 to 256 that reading K again takes, up to
+// this much memory.
+constexpr size_t kMostScores = (size_t)1 << 30;
 struct Plan {
     int few;      // columns that the decode kernel takes at most (0: not launched)
     bool chunk;   // is the chunk kernel launched?
     int ntiles;
     PagedParts dec, chk;
+    PagedScores scores;  // x null: not kept
+    bool keep_scores;
     size_t bytes;
 };
 
@@ -240,11 +316,21 @@ Plan make_plan(const PagedAttn& a, char* ws) {
         const long units = (long)p.ntiles * Hkv;
         const int rows = std::min(a.batch.max_new, kChunkCols / G + 1);
         const int E = paged_walk(m, std::max(0, a.batch.max_kv - rows), a.batch.max_kv).E;
-        int S = units >= 512 ? 1 : (int)std::min<long>(32, (768 + units - 1) / units);
+        int S = units >= 256 ? 1 : (int)std::min<long>(32, (512 + units - 1) / units);
         S = std::max(1, std::min(S, (E + 255) / 256));
         p.chk.S = S;
         p.chk.want = S == 1 ? 1 << 24 : std::max(256, (E + S - 1) / S);
         place(p.chk, (size_t)units, kChunkCols);
+    }
+    if (p.few && a.weigh) {
+        p.scores.cols = p.dec.cols;
+        p.scores.pitch = (a.batch.max_kv + 127) / 128 * 128;
+        const size_t n = (size_t)B * Hkv * p.scores.cols * p.scores.pitch * sizeof(float);
+        p.keep_scores = n <= kMostScores;
+        if (p.keep_scores) {
+            p.scores.x = (float*)(ws + off);
+            off += align256(n);
+        }
     }
     p.bytes = std::max<size_t>(off, 256);
     return p;
@@ -270,12 +356,17 @@ hipError_t launch_paged_attn(const PagedAttn& a, bool e4m3, void* ws, hipStream_
     const Plan p = make_plan(a, (char*)ws);
     hipError_t e = hipSuccess;
     if (p.chunk) e = launch_paged_chunk(a, e4m3, p.chk, p.ntiles, p.few, st);
-    if (e == hipSuccess && p.few) e = launch_paged_decode(a, e4m3, p.dec, p.few, st);
+    if (e == hipSuccess && p.few) e = launch_paged_decode(a, e4m3, p.dec, p.keep_scores ? p.scores : PagedScores{}, p.few, st);
     const int D = built_for(a.kv.D);
     if (e == hipSuccess) e = D == 64 ? launch_combine<64>(a, p, st) : D == 96 ? launch_combine<96>(a, p, st) : launch_combine<128>(a, p, st);
     if (e != hipSuccess || !a.weigh) return e;
-    const dim3 grid((a.batch.max_kv + 127) / 128, a.kv.Hkv, a.batch.B);
-    auto go = [&](auto kern) { kern<<<grid, 256, 0, st>>>(a); };
+    if (p.keep_scores) {
+        paged_weigh_few_kernel<<<dim3((a.batch.max_kv + 255) / 256, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, p.scores);
+        e = hipGetLastError();
+        if (e != hipSuccess || !p.chunk) return e;
+    }
+    const int min_cols = p.keep_scores ? p.scores.cols : 0;
+    auto go = [&](auto kern) { kern<<<dim3((a.batch.max_kv + kWeighKeys - 1) / kWeighKeys, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, min_cols); };
     if (D == 64) e4m3 ? go(paged_weigh_kernel<64, true>) : go(paged_weigh_kernel<64, false>);
     else if (D == 96) e4m3 ? go(paged_weigh_kernel<96, true>) : go(paged_weigh_kernel<96, false>);
     else e4m3 ? go(paged_weigh_kernel<128, true>) : go(paged_weigh_kernel<128, false>);

@@ -1,4 +1,6 @@
 // Rows of a paged cache moved about: the new rows of a batch into their pages, and the rows of most weight into new pages.
+#include <algorithm>
+
 #include "paged.h"
 
 namespace unigist {
@@ -49,10 +51,14 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedKv c, PagedBatch
 // ---------------------------------------------------------------------------------------------
 // Eviction, first part: which rows stay.  A workgroup takes one kv head of one sequence.  Rows are ordered by a 32-bit key
 // that grows with the weight (the float's bits, made monotone; protected rows the largest, NaN the least); the keep-th
-// largest key is found digit by digit from histograms in LDS, then one pass in row order numbers the rows above it and
-// as many of those equal to it as are left to take, lowest rows first.
+// largest key is found digit by digit from histograms in LDS, then the rows above it and as many of those equal to it as are
+// left to take, lowest first, are numbered in row order.  Bound by latency: the keys are fetched once, kPer at a time in
+// flight (a page's number, then the weight), and stay in LDS, up to kCached of them (the rest are fetched again in each of
+// the five passes); the numbering takes a contiguous stretch of rows per wave, counted first, so that it needs one barrier.
 constexpr int kSel = 1024;  // threads
 constexpr int kBins = 4096;
+constexpr int kPer = 8;
+constexpr int kCached = 32768;
 
 __device__ __forceinline__ unsigned weight_key(float w) {
     if (w != w) return 0u;
@@ -64,9 +70,11 @@ __device__ __forceinline__ unsigned weight_key(float w) {
 __global__ __launch_bounds__(kSel) void paged_select_kernel(PagedKv c, PagedKv to, const int* __restrict__ kv_len, const int* __restrict__ keep,
                                                             int max_kv, int max_keep, int sinks, int recent, int* __restrict__ kept,
                                                             int* __restrict__ rows_out) {
+    constexpr int kWaves = kSel / 64;
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    extern __shared__ unsigned cache[];  // min(max_kv, kCached) keys
     __shared__ int hist[kBins];
-    __shared__ int part[kSel / 64];
+    __shared__ int part[kWaves], part2[kWaves];
     __shared__ int found, above, bad;
     int* list = kept + ((size_t)b * c.Hkv + h) * max_keep;
     const int len = kv_len[b], want = keep[b];
@@ -85,20 +93,42 @@ __global__ __launch_bounds__(kSel) void paged_select_kernel(PagedKv c, PagedKv t
     for (int i = (refused ? 0 : stay) + tid; i < max_keep; i += kSel) list[i] = -1;
     if (refused || stay == 0) return;
 
-    auto key_of = [&](int j) {
-        if (j < sinks || j >= len - recent) return 0xffffffffu;
-        return weight_key(c.weight[pool_row(c, b, h, j)]);
+    auto is_safe = [&](int j) { return j < sinks || j >= len - recent; };
+    auto fetch = [&](int j0, unsigned (&key)[kPer]) {  // of the rows j0 + kSel * i, those that there are
+        int at[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) at[i] = pool_row(c, b, h, min(j0 + kSel * i, len - 1));
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) key[i] = weight_key(c.weight[at[i]]);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) key[i] = is_safe(j0 + kSel * i) ? 0xffffffffu : key[i];
     };
+    const int cached = min(len, kCached);
+    for (int j0 = tid; j0 < cached; j0 += kSel * kPer) {
+        unsigned key[kPer];
+        fetch(j0, key);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (j0 + kSel * i < cached) cache[j0 + kSel * i] = key[i];
+    }
     unsigned limit = 0u;  // the stay-th largest key
     int left = stay;      // rows still to take among those that share its leading digits
     const int shifts[3] = {20, 10, 0}, bits[3] = {12, 10, 10};
+#pragma unroll 1
     for (int p = 0; p < 3; ++p) {
-        const int bins = 1 << bits[p], up = shifts[p] + bits[p];
+        const int bins = 1 << bits[p], up = shifts[p] + bits[p], down = shifts[p];
         for (int i = tid; i < bins; i += kSel) hist[i] = 0;
         __syncthreads();
-        for (int j = tid; j < len; j += kSel) {
-            const unsigned key = key_of(j);
-            if (up == 32 || (key >> up) == (limit >> up)) atomicAdd(&hist[(key >> shifts[p]) & (bins - 1)], 1);
+        auto count = [&](unsigned key) {
+            if (up == 32 || ((key ^ limit) >> up) == 0u) atomicAdd(&hist[(key >> down) & (bins - 1)], 1);
+        };
+        for (int j = tid; j < cached; j += kSel) count(cache[j]);
+        for (int j0 = cached + tid; j0 < len; j0 += kSel * kPer) {
+            unsigned key[kPer];
+            fetch(j0, key);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (j0 + kSel * i < len) count(key[i]);
         }
         __syncthreads();
         // bins per thread from the top: thread 0 has the largest digits
@@ -126,39 +156,43 @@ __global__ __launch_bounds__(kSel) void paged_select_kernel(PagedKv c, PagedKv t
             }
         }
         __syncthreads();
-        limit |= (unsigned)found << shifts[p];
+        limit |= (unsigned)found << down;
         left -= above;
         __syncthreads();
     }
-    // rows in order: `done` rows numbered so far, `ties` rows equal to the limit met so far
-    int done = 0, ties = 0;
-    for (int j0 = 0; j0 < len; j0 += kSel) {
-        const int j = j0 + tid;
-        const unsigned key = j < len ? key_of(j) : 0u;
-        const bool tie = j < len && key == limit;
-        const unsigned long long before = (1ull << lane) - 1ull;
-        const unsigned long long tb = __builtin_amdgcn_ballot_w64(tie);
-        if (lane == 0) part[wave] = __popcll(tb);
-        __syncthreads();
-        int tie_at = ties + __popcll(tb & before), all_ties = 0;
-        for (int w = 0; w < kSel / 64; ++w) {
-            if (w < wave) tie_at += part[w];
-            all_ties += part[w];
-        }
-        __syncthreads();
-        const bool stays = j < len && (key > limit || (tie && tie_at < left));
-        const unsigned long long sb = __builtin_amdgcn_ballot_w64(stays);
-        if (lane == 0) part[wave] = __popcll(sb);
-        __syncthreads();
-        int at = done + __popcll(sb & before), all = 0;
-        for (int w = 0; w < kSel / 64; ++w) {
-            if (w < wave) at += part[w];
-            all += part[w];
-        }
-        if (stays) list[at] = j;  // at < stay: as many rows pass as stay
-        done += all;
-        ties += all_ties;
-        __syncthreads();
+    // ---- numbering: wave w takes the rows [w * seg, (w + 1) * seg)
+    const int seg = ((len + kWaves - 1) / kWaves + 63) / 64 * 64;
+    const int j0 = wave * seg, j1 = min(len, j0 + seg);
+    auto key_at = [&](int j) {
+        if (j >= j1) return 0u;
+        if (j < cached) return cache[j];
+        return is_safe(j) ? 0xffffffffu : weight_key(c.weight[pool_row(c, b, h, j)]);
+    };
+    int over = 0, ties = 0;  // rows above the limit and at it in the rows of the waves so far
+    for (int j = j0; j < j1; j += 64) {
+        const unsigned key = key_at(j + lane);
+        over += __popcll(__builtin_amdgcn_ballot_w64(key > limit));
+        ties += __popcll(__builtin_amdgcn_ballot_w64(j + lane < j1 && key == limit));
+    }
+    if (lane == 0) {
+        part[wave] = over;
+        part2[wave] = ties;
+    }
+    __syncthreads();
+    over = ties = 0;
+    for (int w = 0; w < wave; ++w) {
+        over += part[w];
+        ties += part2[w];
+    }
+    const unsigned long long before = (1ull << lane) - 1ull;
+    for (int j = j0; j < j1; j += 64) {
+        const unsigned key = key_at(j + lane);
+        const unsigned long long ob = __builtin_amdgcn_ballot_w64(key > limit);
+        const unsigned long long tb = __builtin_amdgcn_ballot_w64(j + lane < j1 && key == limit);
+        const int tie_at = ties + __popcll(tb & before), taken = min(tie_at, left);  // ties in front of this row that are taken
+        if ((ob >> lane & 1) || ((tb >> lane & 1) && tie_at < left)) list[over + __popcll(ob & before) + taken] = j + lane;
+        over += __popcll(ob);
+        ties += __popcll(tb);
     }
 }
 
@@ -191,7 +225,8 @@ hipError_t launch_paged_append(const PagedKv& c, const PagedBatch& x, bool e4m3,
 
 hipError_t launch_paged_evict(const PagedKv& src, const PagedKv& dst, int elem, const int* kv_len, const int* keep, int B, int max_kv,
                               int max_keep, int sinks, int recent, int* kept, int* rows_out, hipStream_t st) {
-    paged_select_kernel<<<dim3(src.Hkv, B), kSel, 0, st>>>(src, dst, kv_len, keep, max_kv, max_keep, sinks, recent, kept, rows_out);
+    const unsigned lds = (unsigned)std::min(max_kv, kCached) * 4u;
+    paged_select_kernel<<<dim3(src.Hkv, B), kSel, lds, st>>>(src, dst, kv_len, keep, max_kv, max_keep, sinks, recent, kept, rows_out);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int row_bytes = src.D * elem;

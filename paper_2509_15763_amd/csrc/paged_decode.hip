@@ -20,7 +20,7 @@ constexpr float kSlack = 8.f;  // the reference is raised when a score exceeds i
 
 // D: built-for head dimension (64, 96, 128), NB: 16-column blocks
 template <int D, bool E4M3, int NB>
-__global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void paged_decode_kernel(PagedAttn a, PagedParts parts) {
+__global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void paged_decode_kernel(PagedAttn a, PagedParts parts, PagedScores scores) {
     constexpr int KS = D / 32, DB = D / 16, CH = D <= 64 ? 8 : 16;  // k-steps, blocks of O^T, 16-byte chunks of an LDS row
     constexpr int NK = E4M3 ? KS / 2 : KS;                          // 16-byte loads of a K row per lane
     constexpr int NH = E4M3 ? KS % 2 : 0;                           // 8-byte ones behind them
@@ -182,6 +182,15 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
 #pragma unroll
                 for (int t = 0; t < 4; ++t) odd |= E4M3 ? not_finite4(x.vw[j][t]) & 0x80808080u : not_finite2(x.vw[j][t]) & 0x80008000u;
         }
+        if (scores.x) {  // base + 31 < pitch: base is a multiple of 32 below the entries, pitch one of 128 no smaller
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                if (16 * nb + r16 < ncol) {
+                    float* x = scores.x + (((size_t)b * a.kv.Hkv + hk) * scores.cols + 16 * nb + r16) * scores.pitch + base + 4 * g4;
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) *(f32x4*)(x + 16 * kb) = sa[nb][kb] * c;
+                }
+        }
         // ---- softmax
         u32x4 pk[NB];
 #pragma unroll
@@ -294,9 +303,9 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
 
 }  // namespace
 
-hipError_t launch_paged_decode(const PagedAttn& a, bool e4m3, const PagedParts& parts, int cols, hipStream_t st) {
+hipError_t launch_paged_decode(const PagedAttn& a, bool e4m3, const PagedParts& parts, const PagedScores& scores, int cols, hipStream_t st) {
     const dim3 grid(parts.S, a.kv.Hkv, a.batch.B);
-    auto go = [&](auto kern) { kern<<<grid, NT, 0, st>>>(a, parts); };
+    auto go = [&](auto kern) { kern<<<grid, NT, 0, st>>>(a, parts, scores); };
     auto pick = [&](auto d) {
         constexpr int D = decltype(d)::value;
         if (cols <= 16) e4m3 ? go(paged_decode_kernel<D, true, 1>) : go(paged_decode_kernel<D, false, 1>);
