@@ -11,51 +11,33 @@ hipError_t launch_paged_chunk(const PagedAttn& a, bool e4m3, const PagedParts& p
 namespace {
 
 // ---------------------------------------------------------------------------------------------
-// Merge of the slices of a column.  W waves a column, each taking every W-th slice; all loads of up to kBatch slices are
-// in flight.  CHUNK: units are tiles of the chunk kernel, else (sequence, kv head) pairs of the decode kernel.
+// Merge of the slices of a column, nothing but latency and the partial results' bytes.  A slice in which the column sees nothing has l = 0
+// and is left out; one with scores that are no numbers has l = NaN and any m.
+__device__ __forceinline__ float slice_weight(f32x2 ml, float mm) {
+    return ml[1] == 0.f ? 0.f : ml[0] == mm ? 1.f : __builtin_amdgcn_exp2f(ml[0] - mm);
+}
+
+// (Sequence, kv head) pairs of the decode kernel: W waves a column, each taking every W-th slice; all loads of up to kBatch
+// slices of a wave are in flight.
 constexpr int kBatch = 8;
-template <int D, int W, bool CHUNK>
-__global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a, PagedParts parts, int limit) {
+template <int D, int W>
+__global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a, PagedParts parts) {
     constexpr int C = (D + 63) / 64;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int part = wave % W, col = blockIdx.x * (4 / W) + wave / W, hk = blockIdx.y;
+    const int part = wave % W, col = blockIdx.x * (4 / W) + wave / W, hk = blockIdx.y, b = blockIdx.z;
     const int Hkv = a.kv.Hkv, G = a.Hq / Hkv;
     __shared__ float sums[4][64 * C];
-    int b = CHUNK ? 0 : blockIdx.z, c0 = 0;
-    if (CHUNK) {
-        const int tile = blockIdx.z;
-        int hi = a.batch.B - 1;
-        while (b < hi) {
-            const int mid = (b + hi + 1) >> 1;
-            const int first = (int)((unsigned)((a.batch.cu ? min(max(a.batch.cu[mid], 0), a.batch.T) : mid) * G) / kChunkCols) + mid;
-            if (first <= tile) b = mid;
-            else hi = mid - 1;
-        }
-    }
     const PagedSeq s = paged_seq(a.batch, b);
     const int ncol = s.n * G;
-    int last = s.len - 1, first = s.p0;  // positions that the slices were made of
-    bool mine;
-    if (CHUNK) {
-        c0 = ((int)blockIdx.z - ((int)((unsigned)(s.t0 * G) / kChunkCols) + b)) * kChunkCols;
-        mine = ncol > limit && c0 >= 0 && c0 < ncol && c0 + col < ncol;
-        const int c1 = min(c0 + kChunkCols, ncol) - 1;
-        first = s.p0 + c0 / G;
-        last = s.p0 + c1 / G;
-    } else {
-        mine = ncol > 0 && ncol <= limit && col < ncol;
-    }
-    const AttnShape m = mask_shape(a.mask);
-    const int E = last >= 0 && mine ? paged_walk(m, max(first, 0), last + 1).E : 0;
-    const int n = paged_slices(E, parts.S, parts.want, CHUNK ? 32 : 128).n;
+    bool mine = ncol <= parts.cols && col < ncol && s.len > 0;
+    const int E = mine ? paged_walk(mask_shape(a.mask), max(s.p0, 0), s.len).E : 0;
+    const int n = paged_slices(E, parts.S, parts.want, 128).n;
     mine = mine && n > 1;
     float acc[C], mm = -INFINITY, ll = 0.f;
 #pragma unroll
-    for (int i = 0; i < C; ++i) acc[i] = 0.f;
+    for (int k = 0; k < C; ++k) acc[k] = 0.f;
     if (mine) {
-        const size_t unit = CHUNK ? (size_t)blockIdx.z * Hkv + hk : (size_t)b * Hkv + hk;
-        const size_t stride = parts.cols;  // columns between slices
-        const size_t at0 = unit * parts.S * stride + col;
+        const size_t stride = parts.cols, at0 = ((size_t)b * Hkv + hk) * parts.S * stride + col;  // columns between slices
         float x[kBatch][C];
         auto load = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
@@ -68,8 +50,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a, PagedPa
         mm = ml[0];
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) mm = fmaxf(mm, __shfl_xor(mm, off, 64));
-        // a slice in which the column sees nothing has l = 0; one with scores that are no numbers l = NaN and any m
-        const float wgt = ml[1] == 0.f ? 0.f : ml[0] == mm ? 1.f : __builtin_amdgcn_exp2f(ml[0] - mm);
+        const float wgt = slice_weight(ml, mm);
         const unsigned long long has = __builtin_amdgcn_ballot_w64(!(ml[1] == 0.f));
         ll = wgt * ml[1];
 #pragma unroll
@@ -95,12 +76,75 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a, PagedPa
         for (int k = 0; k < C; ++k) acc[k] = (sums[wave][64 * k + lane] + sums[wave + 1][64 * k + lane]) + (sums[wave + 2][64 * k + lane] + sums[wave + 3][64 * k + lane]);
     }
     if (!mine) return;
-    const int i = (c0 + col) / G, hq = hk * G + (c0 + col - i * G), t = s.t0 + i;
+    const int i = col / G, hq = hk * G + (col - i * G), t = s.t0 + i;
 #pragma unroll
     for (int k = 0; k < C; ++k)
         if (64 * k + lane < a.kv.D)
             Elem<bf16_t>::store(a.out + (size_t)hq * a.q_hs + (size_t)t * a.q_rs + 64 * k + lane, ll == 0.f ? 0.f : acc[k] / ll);
     if (lane == 0 && a.lse) a.lse[(size_t)hq * a.batch.T + t] = ll == 0.f ? -INFINITY : mm * kLn2 + __builtin_amdgcn_logf(ll) * kLn2;
+}
+
+// Tiles of the chunk kernel: 16 columns a workgroup, 16 lanes a column (a lane has the columns 4 (lane % 16) + 64 k .. + 3 of
+// D), eight slices in flight.
+template <int D>
+__global__ __launch_bounds__(256) void paged_combine_chunk_kernel(PagedAttn a, PagedParts parts, int min_cols) {
+    constexpr int C = (D + 63) / 64, NB = 8;
+    const int sub = threadIdx.x & 15, hk = blockIdx.y, tile = blockIdx.z;
+    const int Hkv = a.kv.Hkv, G = a.Hq / Hkv;
+    const int b = seq_of_tile(a.batch, G, tile);
+    const PagedSeq s = paged_seq(a.batch, b);
+    const int ncol = s.n * G, c0 = (tile - first_tile(s.t0, G, b)) * kChunkCols, col = c0 + blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (ncol <= min_cols || c0 < 0 || col >= ncol) return;
+    const int pe = s.p0 + (min(c0 + kChunkCols, ncol) - 1) / G;
+    const int E = pe >= 0 ? paged_walk(mask_shape(a.mask), max(s.p0 + c0 / G, 0), pe + 1).E : 0;
+    const int n = paged_slices(E, parts.S, parts.want, 32).n;
+    if (n <= 1) return;
+    const size_t at0 = (((size_t)tile * Hkv + hk) * parts.S) * kChunkCols + (col - c0);
+    const f32x2* ml = (const f32x2*)parts.ml + at0;
+    f32x4 acc[C], x[NB][C];
+    f32x2 y[NB];
+    auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const size_t at = (size_t)min(s0 + i, n - 1) * kChunkCols;
+            y[i] = ml[at];
+#pragma unroll
+            for (int k = 0; k < C; ++k) x[i][k] = *(const f32x4*)(parts.acc + (at0 + at) * D + min(64 * k + 4 * sub, D - 4));
+        }
+    };
+    float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+    for (int k = 0; k < C; ++k) acc[k] = zero4();
+    for (int s0 = 0; s0 < n; s0 += NB) {
+        load(s0);
+        float top = mm;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) top = fmaxf(top, y[i][0]);
+        const float old = slice_weight(f32x2{mm, ll}, top);
+        ll *= old;
+#pragma unroll
+        for (int k = 0; k < C; ++k) acc[k] *= old;
+        mm = top;
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            if (s0 + i < n && !(y[i][1] == 0.f)) {
+                const float f = slice_weight(y[i], mm);
+                ll += f * y[i][1];
+#pragma unroll
+                for (int k = 0; k < C; ++k) acc[k] += f * x[i][k];
+            }
+    }
+    const int i = col / G, hq = hk * G + (col - i * G), t = s.t0 + i;
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll
+    for (int k = 0; k < C; ++k)
+        if (64 * k + 4 * sub < a.kv.D) {
+            u32x2 w2;
+            w2[0] = pack_bf16x2(acc[k][0] * inv, acc[k][1] * inv);
+            w2[1] = pack_bf16x2(acc[k][2] * inv, acc[k][3] * inv);
+            *(u32x2*)(a.out + (size_t)hq * a.q_hs + (size_t)t * a.q_rs + 64 * k + 4 * sub) = w2;
+        }
+    if (sub == 0 && a.lse) a.lse[(size_t)hq * a.batch.T + t] = ll == 0.f ? -INFINITY : mm * kLn2 + __builtin_amdgcn_logf(ll) * kLn2;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -268,6 +312,7 @@ __global__ __launch_bounds__(256) void paged_weigh_few_kernel(PagedAttn a, Paged
 // kernel; a batch that may hold both launches both, and each leaves the other's sequences.
 // Scores of few columns are kept for the weights, 4 bytes a column and key for the 128 to 256 that reading K again takes, up to
 // this much memory.
+constexpr int kOneSlice = 384, kLongSlice = 2048;
 constexpr size_t kMostScores = (size_t)1 << 30;
 struct Plan {
     int few;      // columns that the decode kernel takes at most (0: not launched)
@@ -304,8 +349,8 @@ Plan make_plan(const PagedAttn& a, char* ws) {
     if (p.few) {
         const int E = paged_walk(m, a.batch.max_kv - 1, a.batch.max_kv).E;
         const long units = (long)B * Hkv;
-        int want = (int)std::min<long>((long)E * units / 1024 + 1, 1 << 24);
-        want = std::max(want, units <= 64 ? 128 : 256);
+        int want = (int)std::min<long>(((long)E * units + 255) / 256, kLongSlice);
+        want = std::max(want, E <= kOneSlice ? E : 128);
         want = std::max(want, (E + 63) / 64);
         p.dec.want = (want + 127) / 128 * 128;
         p.dec.S = std::min(64, std::max(1, (E + p.dec.want - 1) / p.dec.want));
@@ -313,10 +358,10 @@ Plan make_plan(const PagedAttn& a, char* ws) {
     }
     if (p.chunk) {
         p.ntiles = (int)((long)T * G / kChunkCols) + B;
-        const long units = (long)p.ntiles * Hkv;
+        const long units = (long)p.ntiles * Hkv, busy = (long)((long)T * G + kChunkCols - 1) / kChunkCols * Hkv;  // workgroups, those with work
         const int rows = std::min(a.batch.max_new, kChunkCols / G + 1);
         const int E = paged_walk(m, std::max(0, a.batch.max_kv - rows), a.batch.max_kv).E;
-        int S = units >= 256 ? 1 : (int)std::min<long>(32, (512 + units - 1) / units);
+        int S = (int)std::min<long>(32, std::max<long>(1, 512 / busy));
         S = std::max(1, std::min(S, (E + 255) / 256));
         p.chk.S = S;
         p.chk.want = S == 1 ? 1 << 24 : std::max(256, (E + S - 1) / S);
@@ -340,11 +385,11 @@ template <int D>
 hipError_t launch_combine(const PagedAttn& a, const Plan& p, hipStream_t st) {
     if (p.few && p.dec.S > 1) {
         const int cols = p.dec.cols;
-        if (p.dec.S > 8) paged_combine_kernel<D, 4, false><<<dim3(cols, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, p.dec, cols);
-        else paged_combine_kernel<D, 1, false><<<dim3((cols + 3) / 4, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, p.dec, cols);
+        if (p.dec.S > kBatch) paged_combine_kernel<D, 4><<<dim3(cols, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, p.dec);
+        else paged_combine_kernel<D, 1><<<dim3((cols + 3) / 4, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, p.dec);
     }
     if (p.chunk && p.chk.S > 1)
-        paged_combine_kernel<D, 1, true><<<dim3(kChunkCols / 4, a.kv.Hkv, p.ntiles), 256, 0, st>>>(a, p.chk, p.few);
+        paged_combine_chunk_kernel<D><<<dim3(kChunkCols / 16, a.kv.Hkv, p.ntiles), 256, 0, st>>>(a, p.chk, p.few);
     return hipGetLastError();
 }
 

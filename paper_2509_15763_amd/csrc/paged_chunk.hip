@@ -42,22 +42,12 @@ __global__ __launch_bounds__(NT, 2) void paged_chunk_kernel(PagedAttn a, PagedPa
     const int r16 = lane & 15, g4 = lane >> 4;
     const int Hkv = a.kv.Hkv, G = a.Hq / Hkv, Dt = a.kv.D;
 
-    // ---- which kv head, slice and tile.  Tiles are numbered from floor(cu[b] * G / 128) + b on for sequence b, which leaves
-    // room for the ceil(n * G / 128) that it has; late tiles, which walk further, first.
+    // ---- which kv head, slice and tile: late tiles, which walk further, first
     const int hk = blockIdx.x % Hkv, rest = blockIdx.x / Hkv;
     const int slice = rest % parts.S, tile = ntiles - 1 - rest / parts.S;
-    int b = 0;
-    {
-        int hi = a.batch.B - 1;
-        while (b < hi) {
-            const int mid = (b + hi + 1) >> 1;
-            const int first = (int)((unsigned)((a.batch.cu ? min(max(a.batch.cu[mid], 0), a.batch.T) : mid) * G) / kChunkCols) + mid;
-            if (first <= tile) b = mid;
-            else hi = mid - 1;
-        }
-    }
+    const int b = seq_of_tile(a.batch, G, tile);
     const PagedSeq s = paged_seq(a.batch, b);
-    const int ncol = s.n * G, c0 = (tile - ((int)((unsigned)(s.t0 * G) / kChunkCols) + b)) * kChunkCols;
+    const int ncol = s.n * G, c0 = (tile - first_tile(s.t0, G, b)) * kChunkCols;
     if (ncol <= min_cols || c0 < 0 || c0 >= ncol) return;
     const AttnShape m = mask_shape(a.mask);
     const int c1 = min(c0 + kChunkCols, ncol) - 1;  // last column
@@ -264,19 +254,16 @@ __global__ __launch_bounds__(NT, 2) void paged_chunk_kernel(PagedAttn a, PagedPa
         l[1] += ls[1];
 
         // ---- O^T += V^T P^T
-        if (careful) {
+        if (careful) {  // apart from the common case, whose reads run ahead of their MFMAs across the blocks
 #pragma unroll
-            for (int qb = 0; qb < 2; ++qb) {
-                f32x4 x[DB];
+            for (int db = 0; db < DB; ++db) {
+                bf16x8 vf = tr16_frag16<CH>(vt + voff[db], 0);
+                careful_v(vf, pk, o[db]);
 #pragma unroll
-                for (int db = 0; db < DB; ++db) x[db] = o[db][qb];
-                careful_pv<DB, CH>(vt, pk[qb], x);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) o[db][qb] = x[db];
+                for (int qb = 0; qb < 2; ++qb) o[db][qb] = mfma16(vf, __builtin_bit_cast(bf16x8, pk[qb]), o[db][qb]);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            return;
-        }
-        {
+        } else {
             constexpr int PFV = 2;
             s16x4 x0[DB], x1[DB];
             auto fetch = [&](int db) __attribute__((always_inline)) {

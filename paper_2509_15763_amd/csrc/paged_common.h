@@ -8,6 +8,23 @@ namespace unigist {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kChunkCols = 128;  // (row, head) columns of a workgroup of the chunk kernel
 
+// Tiles of kChunkCols columns are numbered from floor(t0 * G / kChunkCols) + b on for sequence b, whose first new row is t0: that
+// leaves room for the ceil(n * G / kChunkCols) that it has.
+__device__ __forceinline__ int first_tile(int t0, int G, int b) { return (int)((unsigned)(t0 * G) / kChunkCols) + b; }
+// the sequence that a tile belongs to: the last one whose numbers begin at or below it; 64 sequences a step
+__device__ __forceinline__ int seq_of_tile(const PagedBatch& x, int G, int tile) {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int b0 = 0; b0 < x.B; b0 += 64) {
+        const int b = b0 + lane;
+        const bool below = b < x.B && first_tile(x.cu ? min(max(x.cu[b], 0), x.T) : b, G, b) <= tile;
+        const unsigned long long bits = __builtin_amdgcn_ballot_w64(below);
+        n += __popcll(bits);
+        if (~bits != 0ull) break;
+    }
+    return max(n - 1, 0);
+}
+
 __device__ __forceinline__ unsigned bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
 // Which of the 32 entries from e on does a query at position p see?  gists: bits of the always-visible ones among them
@@ -32,27 +49,32 @@ __device__ __forceinline__ u32x2 widen4(unsigned w) {
     return r;
 }
 
-// O^T += V^T P^T key by key, for a tile of 32 rows of which some hold values that are not finite and some columns do not
-// see all: a product with P = 0 would carry them over.  vt: the tile in LDS (bf16, swizzled); pk: P of a 16-column block
-// as the B operand, zero where a column does not see a key.  Rare, so as small as it can be.
-template <int DB, int CH>
-__device__ __forceinline__ void careful_pv(const char* vt, const u32x4 pk, f32x4 (&o)[DB]) {
-    const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
-#pragma unroll 1
-    for (int key = 0; key < 32; ++key) {
-        const int word = 2 * (key >> 4) + ((key & 3) >> 1);
-        const unsigned mine = word == 0 ? pk[0] : word == 1 ? pk[1] : word == 2 ? pk[2] : pk[3];
-        const unsigned two = (unsigned)__shfl((int)mine, ((key & 15) >> 2) * 16 + r16, 64);
-        const float p = __uint_as_float(key & 1 ? two & 0xffff0000u : two << 16);
+// Before o[..] += V^T P^T (blocks of 16 x 16) where V may hold values that are not finite and some columns do not see all of its
+// rows: a product with P = 0 would carry them over.  What is not finite is counted by products of ones, apart for +inf and
+// -inf (not a number is both), and enters the columns that give it any weight; vf is left with the finite part.
+template <int N>
+__device__ __forceinline__ void careful_v(bf16x8& vf, const u32x4 (&p)[N], f32x4 (&o)[N]) {
+    u32x4 v = __builtin_bit_cast(u32x4, vf), up, down;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const u32x2 v = *(const u32x2*)(vt + key * (CH * 16) + (((2 * db + (g4 >> 1)) ^ swz16<CH>(key)) << 4) + (g4 & 1) * 8);
-            if (p != 0.f) {
-                o[db][0] += p * __uint_as_float(v[0] << 16);
-                o[db][1] += p * __uint_as_float(v[0] & 0xffff0000u);
-                o[db][2] += p * __uint_as_float(v[1] << 16);
-                o[db][3] += p * __uint_as_float(v[1] & 0xffff0000u);
-            }
+    for (int i = 0; i < 4; ++i) {  // two bf16 a word: a truth value is bit 15 or 31
+        const unsigned odd = ((v[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+        const unsigned nan = ((v[i] & 0x007f007fu) + 0x007f007fu) << 8;
+        up[i] = ((odd & (~v[i] | nan)) >> 15) * 0x3f80u;  // 1 in bf16
+        down[i] = ((odd & (v[i] | nan)) >> 15) * 0x3f80u;
+        v[i] &= ~((odd >> 15) * 0xffffu);
+    }
+    vf = __builtin_bit_cast(bf16x8, v);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        u32x4 has;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) has[i] = ((((p[n][i] & 0x7fff7fffu) + 0x7fff7fffu) & 0x80008000u) >> 15) * 0x3f80u;
+        const f32x4 u = mfma16(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, has), zero4());
+        const f32x4 d = mfma16(__builtin_bit_cast(bf16x8, down), __builtin_bit_cast(bf16x8, has), zero4());
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (u[i] > 0.f) o[n][i] += INFINITY;
+            if (d[i] > 0.f) o[n][i] -= INFINITY;
         }
     }
 }

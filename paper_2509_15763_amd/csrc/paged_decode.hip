@@ -18,9 +18,10 @@ namespace {
 constexpr int NT = 256;
 constexpr float kSlack = 8.f;  // the reference is raised when a score exceeds it by 2^kSlack
 
-// D: built-for head dimension (64, 96, 128), NB: 16-column blocks
-template <int D, bool E4M3, int NB>
-__global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void paged_decode_kernel(PagedAttn a, PagedParts parts, PagedScores scores) {
+// D: built-for head dimension (64, 96, 128), FULL: known to be the tensors' too (at 128, where the addresses'
+// registers decide between one and two workgroups per CU), NB: 16-column blocks
+template <int D, bool FULL, bool E4M3, int NB>
+__global__ __launch_bounds__(NT, NB == 1 && (FULL || D < 128 || E4M3) ? (D == 64 ? 3 : 2) : 1) void paged_decode_kernel(PagedAttn a, PagedParts parts, PagedScores scores) {
     constexpr int KS = D / 32, DB = D / 16, CH = D <= 64 ? 8 : 16;  // k-steps, blocks of O^T, 16-byte chunks of an LDS row
     constexpr int NK = E4M3 ? KS / 2 : KS;                          // 16-byte loads of a K row per lane
     constexpr int NH = E4M3 ? KS % 2 : 0;                           // 8-byte ones behind them
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
     // ---- columns: B operand Q^T, positions
     bf16x8 qf[NB][KS];
     int pos[NB], lo[NB];
-    const int Dt = a.kv.D;
+    const int Dt = FULL ? D : a.kv.D;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const int col = min(16 * nb + r16, ncol - 1), i = col / G, h = col - i * G;  // columns past the end shadow the last
@@ -67,12 +68,12 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
         }
     }
     const int lo_last = p_last >= 0 ? win_lo(m, p_last) : 0;
-    f32x4 o[NB][DB];
+    f32x4 o[DB][NB];
     float mr[NB], l[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[nb][db] = zero4();
+        for (int db = 0; db < DB; ++db) o[db][nb] = zero4();
         mr[nb] = -INFINITY;
         l[nb] = 0.f;
     }
@@ -83,11 +84,16 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
 #pragma unroll
     for (int db = 0; db < DB; ++db) toff[db] = tr16_lane_off16<CH>(db);
     // pieces that a row does not have: its first one again (their q is zero, their columns of O are not stored)
-    const char *kl[NK > 0 ? NK : 1], *kh = a.kv.k;
+    auto piece = [&](int at) { return FULL || at < row_bytes ? at : 0; };
+    const char* kl[FULL ? 1 : NK + NH];  // FULL: piece t lies at a constant distance
+    const char* kh = a.kv.k + piece(64 * NK + 8 * g4);
+    if constexpr (FULL) {
+        kl[0] = a.kv.k + 16 * g4;
+    } else {
 #pragma unroll
-    for (int t = 0; t < NK; ++t) kl[t] = a.kv.k + (64 * t + 16 * g4 < row_bytes ? 64 * t + 16 * g4 : 0);
-    if (NH) kh += 64 * NK + 8 * g4 < row_bytes ? 64 * NK + 8 * g4 : 0;
-    const char* vl = a.kv.v + (16 * (lane % LPR) < row_bytes ? 16 * (lane % LPR) : 0);
+        for (int t = 0; t < NK; ++t) kl[t] = a.kv.k + piece(64 * t + 16 * g4);
+    }
+    const char* vl = a.kv.v + piece(16 * (lane % LPR));
 
     // ---- places: of the entries `base` + lane (lanes 0 .. 31) and `base` + 96 + lane, i.e. of this iteration and the next
     unsigned* pl = &places[w][0][0];
@@ -108,7 +114,7 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
         for (int kb = 0; kb < 2; ++kb) {
             const size_t off = (size_t)at[16 * kb + r16] << 4;
 #pragma unroll
-            for (int t = 0; t < NK; ++t) x.kw[kb][t] = *(const u32x4*)(kl[t] + off);
+            for (int t = 0; t < NK; ++t) x.kw[kb][t] = *(const u32x4*)((FULL ? kl[0] + 64 * t : kl[t]) + off);
             if (NH) x.kx[kb] = *(const u32x2*)(kh + off);
         }
         unsigned vo[NLV];
@@ -206,7 +212,7 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
 #pragma unroll
                     for (int db = 0; db < DB; ++db)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[nb][db][i] *= alpha;
+                        for (int i = 0; i < 4; ++i) o[db][nb][i] *= alpha;
                     mr[nb] = mx;
                 }
             }
@@ -221,16 +227,13 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
             for (int t = 0; t < 4; ++t) pk[nb][t] = pack_bf16x2(p[2 * t], p[2 * t + 1]);
         }
         // ---- O^T += V^T P^T (the tile writes above are this wave's own: LDS operations of a wave complete in order)
-        if (__builtin_amdgcn_ballot_w64(odd != 0u) != 0ull) {
+        const bool careful = __builtin_amdgcn_ballot_w64(odd != 0u) != 0ull;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) careful_pv<DB, CH>(vt, pk[nb], o[nb]);
-        } else {
+        for (int db = 0; db < DB; ++db) {
+            bf16x8 vf = tr16_frag16<CH>(vt + toff[db], 0);
+            if (careful) careful_v(vf, pk, o[db]);
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const bf16x8 vf = tr16_frag16<CH>(vt + toff[db], 0);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) o[nb][db] = mfma16(vf, __builtin_bit_cast(bf16x8, pk[nb]), o[nb][db]);
-            }
+            for (int nb = 0; nb < NB; ++nb) o[db][nb] = mfma16(vf, __builtin_bit_cast(bf16x8, pk[nb]), o[db][nb]);
         }
     };
 
@@ -266,12 +269,13 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
     float* po = psum + 4 * COLS;    // [4 waves][COLS][PD]
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
+        if (16 * nb + r16 >= ncol) continue;
         if (g4 == 0) {
             pm[w * COLS + 16 * nb + r16] = mr[nb];
             psum[w * COLS + 16 * nb + r16] = l[nb];
         }
 #pragma unroll
-        for (int db = 0; db < DB; ++db) *(f32x4*)(po + (w * COLS + 16 * nb + r16) * PD + 16 * db + 4 * g4) = o[nb][db];
+        for (int db = 0; db < DB; ++db) *(f32x4*)(po + (w * COLS + 16 * nb + r16) * PD + 16 * db + 4 * g4) = o[db][nb];
     }
     __syncthreads();
     const float vmul = E4M3 ? a.kv.vscale[hk] : 1.f;
@@ -306,14 +310,16 @@ __global__ __launch_bounds__(NT, E4M3 && NB == 1 ? (D == 64 ? 3 : 2) : 1) void p
 hipError_t launch_paged_decode(const PagedAttn& a, bool e4m3, const PagedParts& parts, const PagedScores& scores, int cols, hipStream_t st) {
     const dim3 grid(parts.S, a.kv.Hkv, a.batch.B);
     auto go = [&](auto kern) { kern<<<grid, NT, 0, st>>>(a, parts, scores); };
-    auto pick = [&](auto d) {
+    auto pick = [&](auto d, auto full) {
         constexpr int D = decltype(d)::value;
-        if (cols <= 16) e4m3 ? go(paged_decode_kernel<D, true, 1>) : go(paged_decode_kernel<D, false, 1>);
-        else e4m3 ? go(paged_decode_kernel<D, true, 2>) : go(paged_decode_kernel<D, false, 2>);
+        constexpr bool FULL = decltype(full)::value;
+        if (cols <= 16) e4m3 ? go(paged_decode_kernel<D, FULL, true, 1>) : go(paged_decode_kernel<D, FULL, false, 1>);
+        else e4m3 ? go(paged_decode_kernel<D, FULL, true, 2>) : go(paged_decode_kernel<D, FULL, false, 2>);
     };
-    if (a.kv.D <= 64) pick(std::integral_constant<int, 64>{});
-    else if (a.kv.D <= 96) pick(std::integral_constant<int, 96>{});
-    else pick(std::integral_constant<int, 128>{});
+    if (a.kv.D <= 64) pick(std::integral_constant<int, 64>{}, std::false_type{});
+    else if (a.kv.D <= 96) pick(std::integral_constant<int, 96>{}, std::false_type{});
+    else if (a.kv.D < 128) pick(std::integral_constant<int, 128>{}, std::false_type{});
+    else pick(std::integral_constant<int, 128>{}, std::true_type{});
     return hipGetLastError();
 }
 
