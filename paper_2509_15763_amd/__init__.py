@@ -28,7 +28,7 @@ from .binding import (  # noqa: F401
     attn_fwd_varlen, attn_bwd_varlen,
     unigist_cache_rows_ex, unigist_cache_update_ex, unigist_prefill_chunk_ex,
     unigist_paged_append, unigist_paged_attn, unigist_paged_attn_workspace, unigist_paged_evict,
-    paged_append, paged_attn, paged_evict,
+    paged_append, paged_attn, paged_evict, PagedKVCache,
     attn_fwd, attn_bwd, decode, n_vis, KVCache, RaggedKVCache, prefill_chunk,
 )
 from .autograd import gist_attention, gist_attention_varlen  # noqa: F401,E402

@@ -4,6 +4,7 @@ computes anything and there is no CPU fallback."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -1138,32 +1139,34 @@ def prefill_chunk(q, cache: "KVCache", r, W, p0, window_mode=UNIGIST_WINDOW_SLID
 def _paged_cache(k, v, table, k_scale, v_scale, weight, values=True):
     """The descriptor of a pool k, v [n_pages, Hkv, page, D] (bf16, or uint8 codes, with scales where values are read or
     written) and a table int32 [B, cols]."""
-    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+    shape, dtype = k.shape, k.dtype
+    if len(shape) != 4 or v.shape != shape or v.dtype != dtype:
         raise UnigistError("k and v must be pools [n_pages, Hkv, page, D] of one shape and dtype")
-    if k.dtype == torch.uint8:
+    n_pages, Hkv, page, D = shape
+    ks = vs = None
+    if dtype == torch.bfloat16:
+        dt = UNIGIST_BF16
+    elif dtype == torch.uint8:
         dt = UNIGIST_E4M3
         if values:
             if k_scale is None or v_scale is None:
                 raise UnigistError("pages of E4M3 codes need k_scale and v_scale")
-            _scales(k_scale, k.shape[1])
-            _scales(v_scale, k.shape[1])
-    elif k.dtype == torch.bfloat16:
-        dt, k_scale, v_scale = UNIGIST_BF16, None, None
+            _scales(k_scale, Hkv)
+            _scales(v_scale, Hkv)
+            ks, vs = k_scale.data_ptr(), v_scale.data_ptr()
     else:
-        raise UnigistError(f"unsupported dtype {k.dtype}: pages hold bf16 or uint8 (E4M3 codes)")
+        raise UnigistError(f"unsupported dtype {dtype}: pages hold bf16 or uint8 (E4M3 codes)")
     if table.dtype != torch.int32 or table.dim() != 2 or table.shape[1] < 1:
         raise UnigistError("table must be int32 [B, cols]")
-    if weight is not None and (weight.dtype != torch.float32 or weight.shape != k.shape[:3]):
+    if weight is not None and (weight.dtype != torch.float32 or weight.shape != shape[:3]):
         raise UnigistError("weight must be float32 [n_pages, Hkv, page]")
     _dev(k, v, table, weight)
-    n_pages, Hkv, page, D = k.shape
-    return _PagedCache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
-                       None if v_scale is None else v_scale.data_ptr(), None if weight is None else weight.data_ptr(),
-                       table.data_ptr(), n_pages, page, table.shape[1], Hkv, D, dt)
+    return _PagedCache(k.data_ptr(), v.data_ptr(), ks, vs, None if weight is None else weight.data_ptr(), table.data_ptr(), n_pages,
+                       page, table.shape[1], Hkv, D, dt)
 
 
 def _int32(t, n, what):
-    if t.dtype != torch.int32 or t.shape != (n,) or not t.is_cuda or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
         raise UnigistError(f"{what} must be int32 [{n}] on the GPU")
     return t.data_ptr()
 
@@ -1189,18 +1192,29 @@ def _rows_view(t, what):
     return t, hs, rs
 
 
-def _same_device(*ts):
-    for t in ts:
-        if t is not None and t.device != ts[0].device:
+def _same_device(first, *others):
+    """All on one device, the current one: the library launches there."""
+    dev = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
             raise UnigistError("tensors must be on one device")
+    if dev != (_device() if _device is not None else torch.cuda.current_device()):
+        raise UnigistError("tensors must be on the current device")
+
+
+@functools.lru_cache(maxsize=4096)
+def _paged_attn_workspace(*sizes):
+    """unigist_paged_attn_workspace by the sizes it depends on (no pointer is followed there)."""
+    n_pages, page, cols, Hkv, D, dt, *rest = sizes
+    c = _PagedCache(256, 256, 256, 256, 256, 256, n_pages, page, cols, Hkv, D, dt)
+    return unigist_paged_attn_workspace(C.byref(c), *rest)
 
 
 def paged_append(k, v, table, kv_len, k_new, v_new, cu=None, k_scale=None, v_scale=None, weight=None):
     """Write the new rows k_new, v_new [Hkv, T, D] (bf16; views such as the transposed one of [T, Hkv, D] are taken
-    as they are) into the pages of a pool k, v
-    [n_pages, Hkv, page, D] (bf16, or uint8: quantised with k_scale, v_scale).  Sequence b's are the rows cu[b] .. cu[b+1]-1
-    (cu int32 [B+1] on the GPU; None: one each) and become the last of its kv_len[b] rows (int32 [B] on the GPU); their
-    weights become 0."""
+    as they are) into the pages of a pool k, v [n_pages, Hkv, page, D] (bf16, or uint8: quantised with k_scale, v_scale).
+    Sequence b's are the rows cu[b] .. cu[b+1]-1 (cu int32 [B+1] on the GPU; None: one each) and become the last of its
+    kv_len[b] rows (int32 [B] on the GPU); their weights become 0."""
     c = _paged_cache(k, v, table, k_scale, v_scale, weight)
     B = table.shape[0]
     if k_new.dim() != 3 or k_new.shape[0] != c.Hkv or k_new.shape[2] != c.D or v_new.shape != k_new.shape:
@@ -1212,19 +1226,19 @@ def paged_append(k, v, table, kv_len, k_new, v_new, cu=None, k_scale=None, v_sca
     if (vhs, vrs) != (hs, rs):
         k_new, hs, rs = _rows_view(k_new.contiguous(), "k_new")
         v_new = _rows_view(v_new.contiguous(), "v_new")[0]
-    _check(unigist_paged_append(C.byref(c), k_new.data_ptr(), v_new.data_ptr(), hs, rs, B, T,
-                                None if cu is None else _int32(cu, B + 1, "cu"), _int32(kv_len, B, "kv_len"), _stream()),
+    _check(load().unigist_paged_append(c, k_new.data_ptr(), v_new.data_ptr(), hs, rs, B, T,
+                                       None if cu is None else _int32(cu, B + 1, "cu"), _int32(kv_len, B, "kv_len"), _stream()),
            "unigist_paged_append")
 
 
 def paged_attn(q, k, v, table, kv_len, r, W, cu=None, max_new=None, max_kv=None, sinks=0, window_mode=UNIGIST_WINDOW_SLIDING,
                k_scale=None, v_scale=None, weight=None, weigh=0, decay=1.0, workspace=None):
     """Attention of the new rows q [Hq, T, D] (bf16; views such as the transposed one of [T, Hq, D] are taken as they are)
-    over a pool of pages that holds their keys already -> out [Hq, T, D] in the same layout, lse [Hq, T].  cu, kv_len: see paged_append.  r, W, sinks, window_mode: the mask of
-    attn_fwd over row numbers; W >= max_kv is plain causal attention.  max_new, max_kv: the most new rows and rows of any sequence
-    (None: whatever the tensors allow; the closer they are, the better the launch fits).  weigh > 0: `weight` (float32
-    [n_pages, Hkv, page]) becomes decay * weight + the attention each row received from the last `weigh` new rows of its
-    sequence.  workspace: a uint8 tensor to reuse, optional."""
+    over a pool of pages that holds their keys already -> out [Hq, T, D] in the same layout, lse [Hq, T].  cu, kv_len: see
+    paged_append.  r, W, sinks, window_mode: the mask of attn_fwd over row numbers; W >= max_kv is plain causal attention.
+    max_new, max_kv: the most new rows and rows of any sequence (None: whatever the tensors allow; the closer they are, the
+    better the launch fits).  weigh > 0: `weight` (float32 [n_pages, Hkv, page]) becomes decay * weight + the attention each
+    row received from the last `weigh` new rows of its sequence.  workspace: a uint8 tensor to reuse, optional."""
     c = _paged_cache(k, v, table, k_scale, v_scale, weight)
     B = table.shape[0]
     if q.dim() != 3 or q.shape[2] != c.D:
@@ -1234,19 +1248,22 @@ def paged_attn(q, k, v, table, kv_len, r, W, cu=None, max_new=None, max_kv=None,
     q, hs, rs = _rows_view(q, "q")
     max_new = (1 if cu is None else max(T, 1)) if max_new is None else int(max_new)
     max_kv = min(c.table_cols * c.page, 1 << 23) if max_kv is None else int(max_kv)
-    sizes = (B, Hq, T)
-    mask = (max_new, max_kv, int(r), int(W), int(sinks), int(window_mode))
-    need = unigist_paged_attn_workspace(C.byref(c), *sizes, *mask, int(weigh))
+    mask, weigh = (max_new, max_kv, int(r), int(W), int(sinks), int(window_mode)), int(weigh)
+    if weigh > 0 and weight is None:
+        raise UnigistError("weigh needs weight")
+    need = _paged_attn_workspace(c.n_pages, c.page, c.table_cols, c.Hkv, D, c.dt, B, Hq, T, *mask, weigh)
     if need == 0:
         raise UnigistError("unigist_paged_attn_workspace: invalid or unsupported arguments")
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    out = torch.empty_strided((Hq, T, D), (hs, rs, 1), dtype=q.dtype, device=q.device)
-    lse = torch.empty(Hq, T, dtype=torch.float32, device=q.device)
-    _check(unigist_paged_attn(C.byref(c), q.data_ptr(), out.data_ptr(), lse.data_ptr(), *sizes,
-                              None if cu is None else _int32(cu, B + 1, "cu"), _int32(kv_len, B, "kv_len"), *mask, hs, rs,
-                              int(weigh), float(decay), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                              _stream()),
+        room = need
+    else:
+        room = workspace.numel() * workspace.element_size()
+    out = torch.empty_strided((Hq, T, D), (hs, rs, 1), dtype=torch.bfloat16, device=q.device)
+    lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device)
+    _check(load().unigist_paged_attn(c, q.data_ptr(), out.data_ptr(), lse.data_ptr(), B, Hq, T,
+                                     None if cu is None else _int32(cu, B + 1, "cu"), _int32(kv_len, B, "kv_len"), *mask, hs, rs,
+                                     weigh, decay, workspace.data_ptr(), room, _stream()),
            "unigist_paged_attn")
     return out, lse
 
@@ -1262,9 +1279,114 @@ def paged_evict(k, v, table, kv_len, weight, keep, k_out, v_out, table_out, max_
     if weight is None or table_out.shape[0] != B or (d.Hkv, d.D, d.dt) != (c.Hkv, c.D, c.dt):
         raise UnigistError("paged_evict needs weights, and a destination of the same batch, heads, head dimension and dtype")
     _same_device(k, v, table, kv_len, weight, keep, k_out, v_out, table_out, weight_out)
-    kept = torch.empty(B, c.Hkv, int(max_keep), dtype=torch.int32, device=k.device)
+    kept = torch.empty((B, c.Hkv, int(max_keep)), dtype=torch.int32, device=k.device)
     rows = torch.empty(B, dtype=torch.int32, device=k.device)
-    _check(unigist_paged_evict(C.byref(c), C.byref(d), B, _int32(kv_len, B, "kv_len"), _int32(keep, B, "keep"), int(max_kv),
-                               int(max_keep), int(sinks), int(recent), kept.data_ptr(), rows.data_ptr(), _stream()),
+    _check(load().unigist_paged_evict(c, d, B, _int32(kv_len, B, "kv_len"), _int32(keep, B, "keep"), int(max_kv), int(max_keep),
+                                      int(sinks), int(recent), kept.data_ptr(), rows.data_ptr(), _stream()),
            "unigist_paged_evict")
     return rows, kept
+
+
+class PagedKVCache:
+    """The pages of a batch of sequences that grow and shrink at their own rates: a pool k, v [n_pages, Hkv, page, D] (bf16, or
+    uint8 codes with k_scale / v_scale), which of its pages are free, and for each of B places a table of pages and a number of
+    rows.  weights=True keeps the attention weight of every row (attend(weigh=...)), by which evict() chooses.  Host-side
+    bookkeeping around paged_append, paged_attn and paged_evict; a step is
+
+        cache.extend(n)                        # n[b] new rows for sequence b: pages, lengths, one copy to the GPU
+        cache.append(k_new, v_new)             # [Hkv, T, D], T = sum(n)
+        out, lse = cache.attend(q, r, W)       # [Hq, T, D]
+    """
+
+    def __init__(self, B, Hkv, n_pages, page, max_rows, D, dtype=torch.bfloat16, device="cuda", k_scale=None, v_scale=None,
+                 weights=False):
+        self.B, self.Hkv, self.page, self.D, self.cols = B, Hkv, int(page), D, -(-int(max_rows) // int(page))
+        self.k_scale, self.v_scale = k_scale, v_scale
+        if dtype == torch.uint8:
+            _scales(k_scale, Hkv)
+            _scales(v_scale, Hkv)
+        self.k, self.v = (torch.empty(n_pages, Hkv, page, D, device=device, dtype=dtype) for _ in range(2))
+        self.weight = torch.zeros(n_pages, Hkv, page, device=device) if weights else None
+        self.free = list(range(n_pages))
+        self.pages, self.rows = [[] for _ in range(B)], [0] * B
+        self.new = [0] * B   # rows added by the last extend
+        self._upload()
+
+    def _upload(self):
+        """Tables, lengths and boundaries of the new rows, in one copy."""
+        B, cols = self.B, self.cols
+        x = torch.full((B * cols + 2 * B + 1,), -1, dtype=torch.int32)
+        for b, p in enumerate(self.pages):
+            x[b * cols:b * cols + len(p)] = torch.tensor(p, dtype=torch.int32)
+        x[B * cols:B * cols + B] = torch.tensor(self.rows, dtype=torch.int32)
+        cu = [0]
+        for n in self.new:
+            cu.append(cu[-1] + n)
+        x[B * cols + B:] = torch.tensor(cu, dtype=torch.int32)
+        x = x.to(self.k.device)
+        self.table, self.kv_len, self.cu = x[:B * cols].view(B, cols), x[B * cols:B * cols + B], x[B * cols + B:]
+
+    def extend(self, n):
+        """n[b] more rows for sequence b; raises, and changes nothing, where a sequence outgrows its table or the pool its pages."""
+        n = [int(x) for x in n]
+        if len(n) != self.B or min(n) < 0:
+            raise UnigistError("extend takes a number of rows for each of the B sequences")
+        need = [-(-(r + m) // self.page) - len(p) for r, m, p in zip(self.rows, n, self.pages)]
+        if any(len(p) + m > self.cols for p, m in zip(self.pages, need)):
+            raise UnigistError("a sequence outgrows max_rows")
+        if sum(need) > len(self.free):
+            raise UnigistError("out of pages")
+        for b, m in enumerate(need):
+            self.pages[b].extend(self.free.pop() for _ in range(m))
+            self.rows[b] += n[b]
+        self.new = n
+        self._upload()
+
+    def append(self, k_new, v_new):
+        """The rows that extend() made room for, [Hkv, sum(n), D] bf16."""
+        paged_append(self.k, self.v, self.table, self.kv_len, k_new, v_new, cu=self.cu, k_scale=self.k_scale, v_scale=self.v_scale,
+                     weight=self.weight)
+
+    def attend(self, q, r, W, sinks=0, window_mode=UNIGIST_WINDOW_SLIDING, weigh=0, decay=1.0, workspace=None):
+        """q [Hq, sum(n), D], the queries of those rows -> out, lse."""
+        return paged_attn(q, self.k, self.v, self.table, self.kv_len, r, W, cu=self.cu, max_new=max(max(self.new), 1),
+                          max_kv=max(max(self.rows), 1), sinks=sinks, window_mode=window_mode, k_scale=self.k_scale,
+                          v_scale=self.v_scale, weight=self.weight, weigh=weigh, decay=decay, workspace=workspace)
+
+    def evict(self, keep, sinks=0, recent=0):
+        """Cut sequence b to keep[b] rows of each kv head (those with more), into new pages; the old ones become free.
+        -> rows (int32 [B]) and their old numbers (int32 [B, Hkv, max(keep)]) on the GPU, as paged_evict; of a sequence that is
+        not cut all its rows."""
+        if self.weight is None:
+            raise UnigistError("evict needs a cache with weights=True")
+        keep = [min(int(x), r) for x, r in zip(keep, self.rows)]
+        if len(keep) != self.B or min(keep) < 0:
+            raise UnigistError("evict takes a number of rows for each of the B sequences")
+        cut = [k < r for k, r in zip(keep, self.rows)]
+        per = [-(-k // self.page) if c else 0 for k, c in zip(keep, cut)]
+        if sum(per) > len(self.free):
+            raise UnigistError("out of pages")
+        fresh = [[self.free.pop() for _ in range(m)] for m in per]
+        to = torch.full((self.B, max(max(per), 1)), -1, dtype=torch.int32)
+        for b, p in enumerate(fresh):
+            to[b, :len(p)] = torch.tensor(p, dtype=torch.int32)
+        # a sequence that is not cut asks for no rows and stays where it is
+        want = torch.tensor([k if c else 0 for k, c in zip(keep, cut)], dtype=torch.int32).to(self.k.device)
+        rows, kept = paged_evict(self.k, self.v, self.table, self.kv_len, self.weight, want, self.k, self.v, to.to(self.k.device),
+                                 max(max(self.rows), 1), max(max(keep), 1), sinks=sinks, recent=recent, weight_out=self.weight)
+        for b, c in enumerate(cut):
+            if c:
+                self.free.extend(self.pages[b])
+                self.pages[b], self.rows[b] = fresh[b], keep[b]
+            else:
+                rows[b] = keep[b]
+                kept[b, :, :keep[b]] = torch.arange(keep[b], dtype=torch.int32, device=kept.device)
+        self.new = [0] * self.B
+        self._upload()
+        return rows, kept
+
+    def release(self, b):
+        """Sequence b is done: its pages become free, its place empty."""
+        self.free.extend(self.pages[b])
+        self.pages[b], self.rows[b], self.new[b] = [], 0, 0
+        self._upload()

@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void paged_combine_chunk_kernel(PagedAttn a, P
 // Bound by the matrix pipe and the exponentials, K is read once.
 constexpr int kWeighKeys = 256, kWeighCols = 64;
 template <int D, bool E4M3>
-__global__ __launch_bounds__(256, 2) void paged_weigh_kernel(PagedAttn a, int min_cols) {
+__global__ __launch_bounds__(256, 3) void paged_weigh_kernel(PagedAttn a, int min_cols) {
     constexpr int KS = D / 32, CH = D <= 64 ? 8 : 16, RPI = 64 / CH, IPW = 16 / RPI;
     __shared__ __attribute__((aligned(1024))) char qs[2][kWeighCols * CH * 16];
     __shared__ float ls[2][kWeighCols];
@@ -333,7 +333,8 @@ Plan make_plan(const PagedAttn& a, char* ws) {
     const int G = a.Hq / a.kv.Hkv, Hkv = a.kv.Hkv, B = a.batch.B, T = a.batch.T, D = built_for(a.kv.D);
     const AttnShape m = mask_shape(a.mask);
     const long most = (long)a.batch.max_new * G;  // columns of a sequence at most
-    p.few = most <= 16 ? 16 : 32;
+    // Where a batch has long chunks, the others are mostly single tokens: 16 columns, two workgroups a CU (32: one), if a token has no more.
+    p.few = most <= 16 || (most > 32 && G <= 16) ? 16 : 32;
     p.chunk = most > p.few;
     if (B == 1 && p.chunk) p.few = 0;
     size_t off = 0;
