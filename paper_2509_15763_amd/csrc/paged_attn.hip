@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void paged_combine_chunk_kernel(PagedAttn a, P
     if (ncol <= min_cols || c0 < 0 || col >= ncol) return;
     const int pe = s.p0 + (min(c0 + kChunkCols, ncol) - 1) / G;
     const int E = pe >= 0 ? paged_walk(mask_shape(a.mask), max(s.p0 + c0 / G, 0), pe + 1).E : 0;
-    const int n = paged_slices(E, parts.S, parts.want, 32).n;
+    const int n = (paged_slices(E, parts.S * parts.groups, parts.want, 32).n + parts.groups - 1) / parts.groups;
     if (n <= 1) return;
     const size_t at0 = (((size_t)tile * Hkv + hk) * parts.S) * kChunkCols + (col - c0);
     const f32x2* ml = (const f32x2*)parts.ml + at0;
@@ -362,10 +362,11 @@ Plan make_plan(const PagedAttn& a, char* ws) {
         const long units = (long)p.ntiles * Hkv, busy = (long)((long)T * G + kChunkCols - 1) / kChunkCols * Hkv;  // workgroups, those with work
         const int rows = std::min(a.batch.max_new, kChunkCols / G + 1);
         const int E = paged_walk(m, std::max(0, a.batch.max_kv - rows), a.batch.max_kv).E;
-        int S = (int)std::min<long>(32, std::max<long>(1, 512 / busy));
-        S = std::max(1, std::min(S, (E + 255) / 256));
+        p.chk.groups = busy <= 256 ? 2 : 1;
+        int S = (int)std::min<long>(32, std::max<long>(1, 256 / busy));
+        S = std::max(1, std::min(S, (E + 511) / 512));
         p.chk.S = S;
-        p.chk.want = S == 1 ? 1 << 24 : std::max(256, (E + S - 1) / S);
+        p.chk.want = S * p.chk.groups == 1 ? 1 << 24 : std::max(256, (E + S * p.chk.groups - 1) / (S * p.chk.groups));
         place(p.chk, (size_t)units, kChunkCols);
     }
     if (p.few && a.weigh) {

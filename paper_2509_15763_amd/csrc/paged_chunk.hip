@@ -8,7 +8,9 @@
 //   bf16: direct global -> LDS loads; codes: through registers, widened once per workgroup on the way.
 // Places: 256 entries (eight steps) at a time, one per thread, into one of two tables in LDS; the table entries of the next
 // 256 are loaded a block ahead and the places of a step are read from LDS one step ahead.
-// Few workgroups: the entries of a tile are shared out in slices, merged by paged_combine_kernel.
+// Few workgroups: a lone wave per SIMD takes about 2000 cycles a step, two together 2200, so the entries of a tile are shared out
+// in slices, two to a workgroup of eight waves (GROUPS, merged through LDS), and from there on to workgroups (merged by
+// paged_combine_chunk_kernel).
 #include "paged_common.h"
 
 namespace unigist {
@@ -29,16 +31,19 @@ struct ChunkSmem {
     unsigned gone[2][kBlock / 32];  // a bit per entry that is not there
 };
 
-template <int D, bool E4M3>
-__global__ __launch_bounds__(NT, 2) void paged_chunk_kernel(PagedAttn a, PagedParts parts, int ntiles, int min_cols) {
+template <int D, bool E4M3, int GROUPS>
+__global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a, PagedParts parts, int ntiles, int min_cols) {
     constexpr int KS = D / 32, DB = D / 16, CH = D <= 64 ? 8 : 16;
     constexpr int RPI = 64 / CH;       // tile rows of one direct load
     constexpr int IPW = BN / RPI / 4;  // direct loads per wave, matrix and tile
     constexpr int PPR = CH / 2;        // 16-code pieces of a row
     constexpr int PCS = BN * PPR;      // pieces of a tile: 256 or 128
-    __shared__ __attribute__((aligned(1024))) ChunkSmem<D> sm;
+    constexpr int kMerge = GROUPS > 1 ? 4 * 64 * (DB * 2 * 16 + 2 * 8) : 0, kStages = GROUPS * (int)sizeof(ChunkSmem<D>);
+    __shared__ __attribute__((aligned(1024))) char smem[kStages > kMerge ? kStages : kMerge];
+    const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+    ChunkSmem<D>& sm = ((ChunkSmem<D>*)smem)[group];
 
-    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x % NT, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);  // inside the group
     const int r16 = lane & 15, g4 = lane >> 4;
     const int Hkv = a.kv.Hkv, G = a.Hq / Hkv, Dt = a.kv.D;
 
@@ -54,10 +59,11 @@ __global__ __launch_bounds__(NT, 2) void paged_chunk_kernel(PagedAttn a, PagedPa
     const int pf = s.p0 + c0 / G, pe = s.p0 + c1 / G;
     PagedWalk walk = {0, 0, 0};
     if (pe >= 0) walk = paged_walk(m, max(pf, 0), pe + 1);
-    const PagedSlices sl = paged_slices(walk.E, parts.S, parts.want, BN);
-    if (slice >= sl.n) return;
-    const int e0 = slice * sl.per, e1 = min(walk.E, e0 + sl.per);
-    const int nsteps = (e1 - e0 + BN - 1) / BN;
+    const PagedSlices sl = paged_slices(walk.E, parts.S * GROUPS, parts.want, BN);
+    if (slice * GROUPS >= sl.n) return;
+    const int e0 = min(walk.E, (slice * GROUPS + group) * sl.per), e1 = min(walk.E, e0 + sl.per);
+    const int nsteps = (e1 - e0 + BN - 1) / BN;  // the first group has no fewer than the second, and both meet at every step
+    const int nmeet = GROUPS > 1 ? (min(walk.E, (slice * GROUPS + 1) * sl.per) - slice * GROUPS * sl.per + BN - 1) / BN : nsteps;
 
     // ---- the wave's columns
     const int cw = c0 + 32 * wv;  // first
@@ -103,7 +109,7 @@ __global__ __launch_bounds__(NT, 2) void paged_chunk_kernel(PagedAttn a, PagedPa
         kl[i] = a.kv.k + off;
         vl[i] = a.kv.v + off;
     }
-    auto row_of = [&](int j) { return entry_row(m, walk, min(e0 + kBlock * j + tid, e1 - 1)); };
+    auto row_of = [&](int j) { return entry_row(m, walk, max(min(e0 + kBlock * j + tid, e1 - 1), 0)); };
     auto put = [&](int j, int id) {
         const PagedPlace p = place_of(a.kv, hk, row_of(j), id, row16);
         sm.places[j & 1][tid] = p.off;
@@ -285,14 +291,14 @@ __global__ __launch_bounds__(NT, 2) void paged_chunk_kernel(PagedAttn a, PagedPa
         }
     };
 
-    if (nsteps > 0) {
+    if (nmeet > 0) {
         put(0, page_id(a.kv, b, row_of(0)));
         int ahead = page_id(a.kv, b, row_of(1));
         __syncthreads();
         places_of(0);
-        issue(0);
+        if (GROUPS == 1 || nsteps > 0) issue(0);
         unsigned gone = __builtin_amdgcn_readfirstlane(gone_next);
-        if (E4M3) land(0);
+        if (E4M3 && (GROUPS == 1 || nsteps > 0)) land(0);
         places_of(1);
         // One step: the other stage is filled for the next one meanwhile.  Places of block j + 1 are written in the middle of block
         // j (whose table is the other one; block j - 1, which this one held, was last read at its last step but one) and first read two steps before the block ends.
@@ -311,12 +317,38 @@ __global__ __launch_bounds__(NT, 2) void paged_chunk_kernel(PagedAttn a, PagedPa
                 gone = __builtin_amdgcn_readfirstlane(gone_next);
                 places_of(it + 2);
             }
-            tile_step(bufc, it, now);
+            if (GROUPS == 1 || it < nsteps) tile_step(bufc, it, now);
             if (E4M3 && more) land(BUF ^ 1);
         };
-        for (int it = 0; it < nsteps; it += 2) {
+        for (int it = 0; it < nmeet; it += 2) {
             one(std::integral_constant<int, 0>{}, it);
-            if (it + 1 < nsteps) one(std::integral_constant<int, 1>{}, it + 1);
+            if (it + 1 < nmeet) one(std::integral_constant<int, 1>{}, it + 1);
+        }
+    }
+
+    if constexpr (GROUPS > 1) {  // the second group's waves leave their part to those of the first: same columns, same lanes
+        f32x4* mo = (f32x4*)smem;                                            // [4 waves][DB][2][64 lanes]
+        f32x2* ml = (f32x2*)(smem + 4 * DB * 2 * 64 * 16);                   // [4 waves][2][64 lanes]
+        __syncthreads();  // the stages are dead
+        if (group == 1) {
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) {
+                ml[(wv * 2 + qb) * 64 + lane] = f32x2{mr[qb], l[qb]};
+#pragma unroll
+                for (int db = 0; db < DB; ++db) mo[((wv * DB + db) * 2 + qb) * 64 + lane] = o[db][qb];
+            }
+        }
+        __syncthreads();
+        if (group == 1) return;
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            const f32x2 x = ml[(wv * 2 + qb) * 64 + lane];
+            const float mm = fmaxf(mr[qb], x[0]);
+            const float f = mr[qb] == mm ? 1.f : __builtin_amdgcn_exp2f((mr[qb] - mm) * c), g = x[0] == mm ? 1.f : __builtin_amdgcn_exp2f((x[0] - mm) * c);
+            l[qb] = l[qb] * f + x[1] * g;
+            mr[qb] = mm;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[db][qb] = o[db][qb] * f + mo[((wv * DB + db) * 2 + qb) * 64 + lane] * g;
         }
     }
 
@@ -330,7 +362,7 @@ __global__ __launch_bounds__(NT, 2) void paged_chunk_kernel(PagedAttn a, PagedPa
         const int col = cw + 16 * qb + r16;
         if (col > c1) continue;
         const float vmul = E4M3 ? a.kv.vscale[hk] : 1.f;
-        if (sl.n > 1) {
+        if (sl.n > GROUPS) {
             const size_t at_col = (((size_t)tile * Hkv + hk) * parts.S + slice) * kChunkCols + (col - c0);
             if (g4 == 0) *(f32x2*)(parts.ml + 2 * at_col) = f32x2{mr[qb] * c, lt};
 #pragma unroll
@@ -357,10 +389,15 @@ __global__ __launch_bounds__(NT, 2) void paged_chunk_kernel(PagedAttn a, PagedPa
 hipError_t launch_paged_chunk(const PagedAttn& a, bool e4m3, const PagedParts& parts, int ntiles, int min_cols, hipStream_t st) {
     const long long blocks = (long long)ntiles * a.kv.Hkv * parts.S;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    auto go = [&](auto kern) { kern<<<dim3((unsigned)blocks), NT, 0, st>>>(a, parts, ntiles, min_cols); };
-    if (a.kv.D <= 64) e4m3 ? go(paged_chunk_kernel<64, true>) : go(paged_chunk_kernel<64, false>);
-    else if (a.kv.D <= 96) e4m3 ? go(paged_chunk_kernel<96, true>) : go(paged_chunk_kernel<96, false>);
-    else e4m3 ? go(paged_chunk_kernel<128, true>) : go(paged_chunk_kernel<128, false>);
+    auto go = [&](auto kern) { kern<<<dim3((unsigned)blocks), NT * parts.groups, 0, st>>>(a, parts, ntiles, min_cols); };
+    auto pick = [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        if (parts.groups == 1) e4m3 ? go(paged_chunk_kernel<D, true, 1>) : go(paged_chunk_kernel<D, false, 1>);
+        else e4m3 ? go(paged_chunk_kernel<D, true, 2>) : go(paged_chunk_kernel<D, false, 2>);
+    };
+    if (a.kv.D <= 64) pick(std::integral_constant<int, 64>{});
+    else if (a.kv.D <= 96) pick(std::integral_constant<int, 96>{});
+    else pick(std::integral_constant<int, 128>{});
     return hipGetLastError();
 }
 
