@@ -5,7 +5,8 @@
 // bound by the cache bytes.  A wave takes 32 entries per iteration, the workgroup's four 128:
 //   S^T = K Q^T     v_mfma_f32_16x16x32_bf16, A = K rows straight from memory (lane r16 + 16 g4: key r16, 16 bytes at 64 t + 16 g4),
 //                   B = Q^T in registers;
-//   softmax         a column is spread over four lanes, its reference is raised lazily, the sum is a per-lane partial;
+//   softmax         a column is spread over four lanes, its reference is raised lazily, the sum is a per-lane partial; no
+//                   maximum is searched in the common iteration;
 //   O^T += V^T P^T  P in place as the B operand; V through a wave-private LDS tile (codes widened) and back transposed.
 // Rows lie wherever the table says.  A wave works out the places of 64 entries (two iterations) at a time, one per lane:
 // the table entries of two pairs ahead are loaded early, and the places go through a wave-private table in LDS from which
@@ -16,7 +17,8 @@ namespace unigist {
 namespace {
 
 constexpr int NT = 256;
-constexpr float kSlack = 8.f;  // the reference is raised when a score exceeds it by 2^kSlack
+constexpr float kSlack = 8.f;       // the reference is raised when a score exceeds it by 2^kSlack
+constexpr float kBigSum = 16384.f;  // a partial sum above this sends the iteration through the maximum search
 
 // D: built-for head dimension (64, 96, 128), FULL: known to be the tensors' too (at 128, where the addresses'
 // registers decide between one and two workgroups per CU), NB: 16-column blocks
@@ -70,6 +72,7 @@ __global__ __launch_bounds__(NT, NB == 1 && (FULL || D < 128 || E4M3) ? (D == 64
     const int lo_last = p_last >= 0 ? win_lo(m, p_last) : 0;
     f32x4 o[DB][NB];
     float mr[NB], l[NB];
+    bool need_max = true;  // until every column of the wave has a reference
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
@@ -197,16 +200,40 @@ __global__ __launch_bounds__(NT, NB == 1 && (FULL || D < 128 || E4M3) ? (D == 64
                     for (int kb = 0; kb < 2; ++kb) *(f32x4*)(x + 16 * kb) = sa[nb][kb] * c;
                 }
         }
-        // ---- softmax
+        // ---- softmax against the running references; only where a partial sum has grown too large, or a column has none yet, the
+        // maximum is searched and the references raised
         u32x4 pk[NB];
+        float ls[NB];
+        auto exps = [&](int nb) __attribute__((always_inline)) {
+            const float mc = (mr[nb] == -INFINITY ? 0.f : mr[nb]) * c;
+            float p[8];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const f32x4 &s0 = sa[nb][0], &s1 = sa[nb][1];
-            float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            if ((mx - mr[nb]) * c > kSlack || mr[nb] == -INFINITY) {  // same decision on the four lanes of a column
-                if (mx > mr[nb]) {
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[4 * kb + i] = __builtin_amdgcn_exp2f(fmaf(sa[nb][kb][i], c, -mc));
+            ls[nb] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+#pragma unroll
+            for (int t = 0; t < 4; ++t) pk[nb][t] = pack_bf16x2(p[2 * t], p[2 * t + 1]);
+        };
+        bool search = need_max;
+        if (!search) {
+            bool big = false;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                exps(nb);
+                big = big || !(ls[nb] <= kBigSum);
+            }
+            search = __builtin_amdgcn_ballot_w64(big) != 0ull;
+        }
+        if (search) {
+            bool none = false;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const f32x4 &s0 = sa[nb][0], &s1 = sa[nb][1];
+                float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+                mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                if ((mx - mr[nb]) * c > kSlack) {  // same decision on the four lanes of a column
                     const float alpha = __builtin_amdgcn_exp2f((mr[nb] - mx) * c);  // m = -inf gives 0
                     l[nb] *= alpha;
 #pragma unroll
@@ -215,17 +242,13 @@ __global__ __launch_bounds__(NT, NB == 1 && (FULL || D < 128 || E4M3) ? (D == 64
                         for (int i = 0; i < 4; ++i) o[db][nb][i] *= alpha;
                     mr[nb] = mx;
                 }
+                exps(nb);
+                none = none || mr[nb] == -INFINITY;
             }
-            const float mc = (mr[nb] == -INFINITY ? 0.f : mr[nb]) * c;
-            float p[8];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[4 * kb + i] = __builtin_amdgcn_exp2f(fmaf(sa[nb][kb][i], c, -mc));
-            l[nb] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-#pragma unroll
-            for (int t = 0; t < 4; ++t) pk[nb][t] = pack_bf16x2(p[2 * t], p[2 * t + 1]);
+            need_max = __builtin_amdgcn_ballot_w64(none) != 0ull;
         }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) l[nb] += ls[nb];
         // ---- O^T += V^T P^T (the tile writes above are this wave's own: LDS operations of a wave complete in order)
         const bool careful = __builtin_amdgcn_ballot_w64(odd != 0u) != 0ull;
 #pragma unroll
