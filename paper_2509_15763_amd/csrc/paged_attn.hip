@@ -149,19 +149,19 @@ __global__ __launch_bounds__(256) void paged_combine_chunk_kernel(PagedAttn a, P
 
 // ---------------------------------------------------------------------------------------------
 // Weights of a sequence of many columns: the scores of the last new rows once more, summed over columns instead of keys.  A
-// wave holds 64 keys of one kv head (A operand K, in registers); the columns come in chunks of 64 through two LDS stages
+// wave holds 128 keys of one kv head (A operand K, in registers); the columns come in chunks of 64 through two LDS stages
 // (B operand Q^T, direct loads, chunks swizzled as in the attention kernels) with their position, the start of their window
 // and their lse, and exp(score - lse) of the visible pairs adds up per lane, over a lane's 16 columns at the end.
 // Bound by the matrix pipe and the exponentials, K is read once.
-constexpr int kWeighKeys = 256, kWeighCols = 64;
+constexpr int kWeighKeys = 512, kWeighCols = 64;
 template <int D, bool E4M3>
-__global__ __launch_bounds__(256, 3) void paged_weigh_kernel(PagedAttn a, int min_cols) {
+__global__ __launch_bounds__(256, 2) void paged_weigh_kernel(PagedAttn a, int min_cols) {
     constexpr int KS = D / 32, CH = D <= 64 ? 8 : 16, RPI = 64 / CH, IPW = 16 / RPI;
     __shared__ __attribute__((aligned(1024))) char qs[2][kWeighCols * CH * 16];
     __shared__ float ls[2][kWeighCols];
     __shared__ int ps[2][kWeighCols], los[2][kWeighCols];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g4 = lane >> 4;
-    const int hk = blockIdx.y, b = blockIdx.z, wg0 = blockIdx.x * kWeighKeys, j0 = wg0 + 64 * w;
+    const int hk = blockIdx.y, b = blockIdx.z, wg0 = blockIdx.x * kWeighKeys, j0 = wg0 + 128 * w;
     const int G = a.Hq / a.kv.Hkv, Dt = a.kv.D;
     const PagedSeq s = paged_seq(a.batch, b);
     const int ncol = s.n * G;
@@ -170,16 +170,23 @@ __global__ __launch_bounds__(256, 3) void paged_weigh_kernel(PagedAttn a, int mi
     const float c = a.scale * (E4M3 ? a.kv.kscale[hk] : 1.f) * kLog2e;
 
     // ---- this wave's keys
-    bf16x8 kf[4][KS];
+    bf16x8 kf[2][4][KS];  // keys j0 + 64 half + 16 kb + r16
     const int row_bytes = Dt * (E4M3 ? 1 : 2), row16 = row_bytes / 16;
-    unsigned long long gone;
-    {
-        const int j = min(j0 + lane, s.len - 1);
-        const PagedPlace mine = place_of(a.kv, hk, j, page_id(a.kv, b, j), row16);
-        gone = __builtin_amdgcn_ballot_w64(!mine.there || j0 + lane >= s.len);
+    unsigned long long gone[2];
+    PagedPlace mine[2];
+    int id[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) id[half] = page_id(a.kv, b, min(j0 + 64 * half + lane, s.len - 1));
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        mine[half] = place_of(a.kv, hk, min(j0 + 64 * half + lane, s.len - 1), id[half], row16);
+        gone[half] = __builtin_amdgcn_ballot_w64(!mine[half].there || j0 + 64 * half + lane >= s.len);
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
-            const char* p = a.kv.k + ((size_t)(unsigned)__shfl((int)mine.off, 16 * kb + r16, 64) << 4);
+            const char* p = a.kv.k + ((size_t)(unsigned)__shfl((int)mine[half].off, 16 * kb + r16, 64) << 4);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const int e = 32 * ks + 8 * g4;
@@ -193,11 +200,10 @@ __global__ __launch_bounds__(256, 3) void paged_weigh_kernel(PagedAttn a, int mi
                         x = *(const u32x4*)(p + 2 * e);
                     }
                 }
-                kf[kb][ks] = __builtin_bit_cast(bf16x8, x);
+                kf[half][kb][ks] = __builtin_bit_cast(bf16x8, x);
             }
         }
-    }
-    float sum[4][4] = {};
+    float sum[2][4][4] = {};
 
     // ---- columns, from the first new row that counts and sees any of these keys
     const int i0 = max(max(0, s.n - a.weigh), wg0 - s.p0);
@@ -239,48 +245,56 @@ __global__ __launch_bounds__(256, 3) void paged_weigh_kernel(PagedAttn a, int mi
                 if (D > Dt && 32 * ks + 8 * g4 >= Dt) x = u32x4{0u, 0u, 0u, 0u};
                 qf[ks] = __builtin_bit_cast(bf16x8, x);
             }
-            f32x4 sa[4];
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb) {
-                sa[kb] = zero4();
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) sa[kb] = mfma16(kf[kb][ks], qf[ks], sa[kb]);
-            }
-            if (gone != 0ull || __builtin_amdgcn_ballot_w64(p < j0 + 63 || lo > j0) != 0ull) {
-                unsigned gists[2] = {0u, 0u};
-                if (__builtin_amdgcn_ballot_w64(p >= 0 && lo > j0) != 0ull) {
-                    const unsigned long long g = __builtin_amdgcn_ballot_w64(is_always(m, j0 + lane));
-                    gists[0] = (unsigned)g;
-                    gists[1] = (unsigned)(g >> 32);
-                }
+            for (int half = 0; half < 2; ++half) {
+                const int jh = j0 + 64 * half;
+                f32x4 sa[4];
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb) {
-                    const int j = j0 + 32 * (kb / 2);
-                    const unsigned vis = p < 0 ? 0u : (bits_below(p - j + 1) & (~bits_below(lo - j) | gists[kb / 2]) & ~(unsigned)(gone >> (32 * (kb / 2))));
+                    sa[kb] = zero4();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!((vis >> (16 * (kb % 2) + 4 * g4 + i)) & 1u)) sa[kb][i] = -INFINITY;
+                    for (int ks = 0; ks < KS; ++ks) sa[kb] = mfma16(kf[half][kb][ks], qf[ks], sa[kb]);
                 }
+                if (gone[half] != 0ull || __builtin_amdgcn_ballot_w64(p < jh + 63 || lo > jh) != 0ull) {
+                    unsigned gists[2] = {0u, 0u};
+                    if (__builtin_amdgcn_ballot_w64(p >= 0 && lo > jh) != 0ull) {
+                        const unsigned long long g = __builtin_amdgcn_ballot_w64(is_always(m, jh + lane));
+                        gists[0] = (unsigned)g;
+                        gists[1] = (unsigned)(g >> 32);
+                    }
+#pragma unroll
+                    for (int kb = 0; kb < 4; ++kb) {
+                        const int j = jh + 32 * (kb / 2);
+                        const unsigned vis =
+                            p < 0 ? 0u : (bits_below(p - j + 1) & (~bits_below(lo - j) | gists[kb / 2]) & ~(unsigned)(gone[half] >> (32 * (kb / 2))));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!((vis >> (16 * (kb % 2) + 4 * g4 + i)) & 1u)) sa[kb][i] = -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[half][kb][i] += __builtin_amdgcn_exp2f(fmaf(sa[kb][i], c, -l2));
             }
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum[kb][i] += __builtin_amdgcn_exp2f(fmaf(sa[kb][i], c, -l2));
         }
     }
-    if (j0 >= s.len) return;
-    float own = 0.f;  // lane r16 ends with the key 16 (r16 / 4) + 4 g4 + r16 % 4
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb)
+    for (int half = 0; half < 2; ++half) {
+        float own = 0.f;  // lane r16 ends with the key 16 (r16 / 4) + 4 g4 + r16 % 4
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-            for (int off = 1; off < 16; off <<= 1) sum[kb][i] += __shfl_xor(sum[kb][i], off, 64);
-            if (r16 == 4 * kb + i) own = sum[kb][i];
-        }
-    const int j = j0 + 16 * (r16 >> 2) + 4 * g4 + (r16 & 3);
-    const int at = j < s.len ? pool_row(a.kv, b, hk, j) : -1;
-    if (at >= 0) a.kv.weight[at] = a.decay == 0.f ? own : fmaf(a.decay, a.kv.weight[at], own);
+            for (int i = 0; i < 4; ++i) {
+                float x = sum[half][kb][i];
+#pragma unroll
+                for (int off = 1; off < 16; off <<= 1) x += __shfl_xor(x, off, 64);
+                if (r16 == 4 * kb + i) own = x;
+            }
+        const int j = j0 + 64 * half + 16 * (r16 >> 2) + 4 * g4 + (r16 & 3);
+        const int at = j < s.len ? pool_row(a.kv, b, hk, j) : -1;
+        if (at >= 0) a.kv.weight[at] = a.decay == 0.f ? own : fmaf(a.decay, a.kv.weight[at], own);
+    }
 }
 
 // Weights of a sequence of few columns, from the scores that the decode kernel has left: one lane per row.
