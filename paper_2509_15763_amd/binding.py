@@ -1303,6 +1303,8 @@ class PagedKVCache:
         self.B, self.Hkv, self.page, self.D, self.cols = B, Hkv, int(page), D, -(-int(max_rows) // int(page))
         self.k_scale, self.v_scale = k_scale, v_scale
         if dtype == torch.uint8:
+            if k_scale is None or v_scale is None:
+                raise UnigistError("pages of E4M3 codes need k_scale and v_scale")
             _scales(k_scale, Hkv)
             _scales(v_scale, Hkv)
         self.k, self.v = (torch.empty(n_pages, Hkv, page, D, device=device, dtype=dtype) for _ in range(2))

@@ -79,7 +79,7 @@ extern "C" unigist_status unigist_paged_append(const unigist_paged_cache* c, con
     if (T == 0) return UNIGIST_OK;
     if (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new)) return UNIGIST_EINVAL;
     if (head_stride % 8 != 0 || row_stride % 8 != 0 || row_stride < c->D || head_stride < 0) return UNIGIST_EINVAL;
-    if (row_stride > 0x7fffffffLL) return UNIGIST_EUNSUPPORTED;
+    if (row_stride > 0x7fffffffLL || (long long)T * c->Hkv > 0x7fffffffLL - 16) return UNIGIST_EUNSUPPORTED;
     const PagedBatch x = {cu, kv_len, B, T, T, kMaxPagedRows};
     hipError_t e = launch_paged_append(kv, x, c->dt == UNIGIST_E4M3, (const bf16_t*)k_new, (const bf16_t*)v_new, head_stride, (int)row_stride,
                                        (hipStream_t)hip_stream);

@@ -89,11 +89,11 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a, PagedPa
 template <int D>
 __global__ __launch_bounds__(256) void paged_combine_chunk_kernel(PagedAttn a, PagedParts parts, int min_cols) {
     constexpr int C = (D + 63) / 64, NB = 8;
-    const int sub = threadIdx.x & 15, hk = blockIdx.y, tile = blockIdx.z;
+    const int sub = threadIdx.x & 15, hk = blockIdx.y, tile = blockIdx.x;
     const int Hkv = a.kv.Hkv, G = a.Hq / Hkv;
     const int b = seq_of_tile(a.batch, G, tile);
     const PagedSeq s = paged_seq(a.batch, b);
-    const int ncol = s.n * G, c0 = (tile - first_tile(s.t0, G, b)) * kChunkCols, col = c0 + blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int ncol = s.n * G, c0 = (tile - first_tile(s.t0, G, b)) * kChunkCols, col = c0 + blockIdx.z * 16 + (threadIdx.x >> 4);
     if (ncol <= min_cols || c0 < 0 || col >= ncol) return;
     const int pe = s.p0 + (min(c0 + kChunkCols, ncol) - 1) / G;
     const int E = pe >= 0 ? paged_walk(mask_shape(a.mask), max(s.p0 + c0 / G, 0), pe + 1).E : 0;
@@ -268,14 +268,17 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(PagedAttn a, int mi
                         const unsigned vis =
                             p < 0 ? 0u : (bits_below(p - j + 1) & (~bits_below(lo - j) | gists[kb / 2]) & ~(unsigned)(gone[half] >> (32 * (kb / 2))));
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (!((vis >> (16 * (kb % 2) + 4 * g4 + i)) & 1u)) sa[kb][i] = -INFINITY;
+                        for (int i = 0; i < 4; ++i) {  // an lse that is no number concerns the keys its row sees and no others
+                            const float x = __builtin_amdgcn_exp2f(fmaf(sa[kb][i], c, -l2));
+                            sum[half][kb][i] += (vis >> (16 * (kb % 2) + 4 * g4 + i)) & 1u ? x : 0.f;
+                        }
                     }
+                } else {
+#pragma unroll
+                    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sum[half][kb][i] += __builtin_amdgcn_exp2f(fmaf(sa[kb][i], c, -l2));
                 }
-#pragma unroll
-                for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[half][kb][i] += __builtin_amdgcn_exp2f(fmaf(sa[kb][i], c, -l2));
             }
         }
     }
@@ -315,7 +318,8 @@ __global__ __launch_bounds__(256) void paged_weigh_few_kernel(PagedAttn a, Paged
         for (int i = max(0, s.n - a.weigh); i < s.n; ++i)
             for (int g = 0; g < G; ++g) {
                 const float lse = a.lse[(size_t)(hk * G + g) * a.batch.T + s.t0 + i];
-                if (lse != -INFINITY) sum += __builtin_amdgcn_exp2f(fmaf(-lse, kLog2e, x[(size_t)(i * G + g) * scores.pitch]));
+                const float y = x[(size_t)(i * G + g) * scores.pitch];
+                if (lse != -INFINITY && y != -INFINITY) sum += __builtin_amdgcn_exp2f(fmaf(-lse, kLog2e, y));
             }
     }
     a.kv.weight[at] = a.decay == 0.f ? sum : fmaf(a.decay, a.kv.weight[at], sum);
@@ -405,7 +409,7 @@ hipError_t launch_combine(const PagedAttn& a, const Plan& p, hipStream_t st) {
         else paged_combine_kernel<D, 1><<<dim3((cols + 3) / 4, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, p.dec);
     }
     if (p.chunk && p.chk.S > 1)
-        paged_combine_chunk_kernel<D><<<dim3(kChunkCols / 16, a.kv.Hkv, p.ntiles), 256, 0, st>>>(a, p.chk, p.few);
+        paged_combine_chunk_kernel<D><<<dim3(p.ntiles, a.kv.Hkv, kChunkCols / 16), 256, 0, st>>>(a, p.chk, p.few);
     return hipGetLastError();
 }
 

@@ -7,17 +7,15 @@ namespace {
 __device__ __forceinline__ float clamp448(float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); }
 
 // ---------------------------------------------------------------------------------------------
-// Append.  A lane moves 8 elements (16 bytes of bf16): D / 8 lanes a row, K and V of it.  Codes are RNE(clamp(x / scale,
-// +-448)) with one correctly rounded division, as unigist_quantize_e4m3 makes them.
+// Append.  A lane moves 8 elements (16 bytes of bf16), 16 lanes a row (those that a smaller head dimension has), K and V of
+// it.  Bound by the rows' bytes; for a token a sequence by latency.  Codes are RNE(clamp(x / scale, +-448)) with one correctly
+// rounded division, as unigist_quantize_e4m3 makes them.
 template <bool E4M3>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedKv c, PagedBatch x, const bf16_t* __restrict__ k_new,
                                                            const bf16_t* __restrict__ v_new, long long hs, int rs) {
-    const int per_row = c.D / 8;
-    const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long row_id = idx / per_row;
-    const int d = (int)(idx - row_id * per_row) * 8;
-    const int t = (int)(row_id / c.Hkv), h = (int)(row_id - (long long)t * c.Hkv);
-    if (t >= x.T) return;
+    const int row_id = blockIdx.x * 16 + threadIdx.x / 16, d = (threadIdx.x & 15) * 8;
+    const int t = row_id / c.Hkv, h = row_id - t * c.Hkv;
+    if (t >= x.T || d >= c.D) return;
     const int b = seq_of_row(x, t);
     const PagedSeq s = paged_seq(x, b);
     if (t < s.t0 || t >= s.t0 + s.n) return;  // behind the last sequence
@@ -225,8 +223,7 @@ __global__ __launch_bounds__(kSel) void paged_select_kernel(PagedKv c, PagedKv t
 __global__ __launch_bounds__(256) void paged_gather_kernel(PagedKv c, PagedKv to, int row_bytes, int max_keep, const int* __restrict__ kept,
                                                            const int* __restrict__ rows_out) {
     const int h = blockIdx.y, b = blockIdx.z, per_row = row_bytes / 16;
-    const int i = (int)(((long long)blockIdx.x * 256 + threadIdx.x) / per_row);
-    const int o = (int)(((long long)blockIdx.x * 256 + threadIdx.x) - (long long)i * per_row) * 16;
+    const int at_lane = blockIdx.x * 256 + threadIdx.x, i = at_lane / per_row, o = (at_lane - i * per_row) * 16;  // 2^23 rows of 16 at most
     if (i >= rows_out[b]) return;  // -1 for a sequence left alone
     const int j = kept[((size_t)b * c.Hkv + h) * max_keep + i];
     const int from = pool_row(c, b, h, j), at = pool_row(to, b, h, i);
@@ -241,10 +238,9 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedKv c, PagedKv to
 
 hipError_t launch_paged_append(const PagedKv& c, const PagedBatch& x, bool e4m3, const bf16_t* k_new, const bf16_t* v_new, long long hs,
                                int rs, hipStream_t st) {
-    const long long lanes = (long long)x.T * c.Hkv * (c.D / 8), blocks = (lanes + 255) / 256;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    if (e4m3) paged_append_kernel<true><<<dim3((unsigned)blocks), 256, 0, st>>>(c, x, k_new, v_new, hs, rs);
-    else paged_append_kernel<false><<<dim3((unsigned)blocks), 256, 0, st>>>(c, x, k_new, v_new, hs, rs);
+    const unsigned blocks = (unsigned)(((long long)x.T * c.Hkv + 15) / 16);
+    if (e4m3) paged_append_kernel<true><<<dim3(blocks), 256, 0, st>>>(c, x, k_new, v_new, hs, rs);
+    else paged_append_kernel<false><<<dim3(blocks), 256, 0, st>>>(c, x, k_new, v_new, hs, rs);
     return hipGetLastError();
 }
 

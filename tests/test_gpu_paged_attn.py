@@ -333,3 +333,65 @@ def test_results_repeat_bit_for_bit_and_on_other_streams():
         again = run(c, 4, 300, weight=c.weight, weigh=8, decay=0.0)
     torch.cuda.synchronize()
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1]) and torch.equal(w, c.weight)
+
+
+def test_a_query_that_is_no_number_concerns_what_it_sees():
+    # new row 1 of 3 (decode) and of 200 (chunk) is NaN: its own outputs, and the weights of the rows up to its position
+    for news in ([3], [200]):
+        case = Paged([400], news, 16, 4, 2, 128, seed=19)
+        clean = case.cuda()
+        want, _ = run(clean, 4, ALL, weight=clean.weight, weigh=1 << 20, decay=0.0)
+        case.q[1, 0] = float("nan")  # one of the two heads of kv head 0
+        c = case.cuda()
+        out, lse = run(c, 4, ALL, weight=c.weight, weigh=1 << 20, decay=0.0)
+        assert torch.isnan(out[0, 1].float()).all() and torch.isnan(lse[0, 1])
+        out[0, 1], want[0, 1] = 0, 0
+        assert torch.equal(out, want)
+        p = 400 - news[0] + 1
+        for j in range(400):
+            pg, slot = int(case.table[0, j // 16]), j % 16
+            assert bool(torch.isnan(c.weight[pg, 0, slot])) == (j <= p)
+            assert abs(float(c.weight[pg, 1, slot]) - float(clean.weight[pg, 1, slot])) <= 1e-6
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_many_tiles_agree_with_the_training_kernel(e4m3):
+    # more tiles than CUs: every row of a sequence against the forward kernel, and the weights against those of a slice of its rows
+    L, page, Hq, Hkv, D, r, W = 9000, 64, 8, 2, 128, 4, 700
+    q, k, v, _ = synth.attn_inputs(1, Hq, Hkv, L, D, seed=20, device="cuda")
+    scales = {}
+    if e4m3:
+        ks, vs = synth.e4m3_scales(Hkv, 2, device="cuda")
+        k8, v8 = u.quantize_e4m3(k, ks), u.quantize_e4m3(v, vs)
+        wide = lambda c, s: (c.view(torch.float8_e4m3fn).float() * s[:, None, None]).to(torch.bfloat16)
+        k, v, scales = wide(k8, ks), wide(v8, vs), dict(k_scale=ks, v_scale=vs)  # rounds where code * scale is no bf16 value
+    n_pages = -(-L // page)
+
+    def pages(x):
+        return torch.nn.functional.pad(x[0], (0, 0, 0, n_pages * page - L)).view(Hkv, n_pages, page, D).transpose(0, 1).contiguous()
+
+    kp, vp = (pages(k8), pages(v8)) if e4m3 else (pages(k), pages(v))
+    table = torch.arange(n_pages, dtype=torch.int32, device="cuda")[None]
+    kv, cu = torch.tensor([L], dtype=torch.int32, device="cuda"), torch.tensor([0, L], dtype=torch.int32, device="cuda")
+    for mask in (dict(), dict(sinks=5), dict(sinks=3, window_mode=1)):
+        WW = 40 if mask.get("window_mode") else W
+        full, flse = u.attn_fwd(q, k, v, r, WW, **mask)
+        weight = torch.zeros(n_pages, Hkv, page, device="cuda")
+        out, lse = u.paged_attn(q[0], kp, vp, table, kv, r, WW, cu=cu, max_new=L, max_kv=L, weight=weight, weigh=300, **mask, **scales)
+        # codes: the forward reads k and v rounded to bf16, 2^-9 of each product's size on either side
+        assert max_abs(to_np(out), to_np(full[0])) <= (3 if e4m3 else 1) * TOL_OUT_BF16
+        assert max_abs(to_np(lse), to_np(flse[0])) <= (1e-2 if e4m3 else TOL_LSE_BF16)
+        assert abs(float(weight.double().sum()) - 300 * Hq) <= 300 * Hq * 2e-4
+        w2 = torch.zeros_like(weight)
+        c2 = torch.tensor([0, 300], dtype=torch.int32, device="cuda")
+        u.paged_attn(q[0, :, L - 300:], kp, vp, table, kv, r, WW, cu=c2, max_new=300, max_kv=L, weight=w2, weigh=300, **mask, **scales)
+        assert float((weight - w2).abs().max()) <= 2e-4 * float(weight.max())
+
+
+def test_hundreds_of_sequences():
+    # more sequences than a wave has lanes: tokens, drafts and chunks side by side
+    lens, news = [], []
+    for b in range(150):
+        news.append((1, 1, 3, 40, 0, 9)[b % 6])
+        lens.append(news[-1] + (b * 37) % 200)
+    check(Paged(lens, news, 16, 4, 2, 64, seed=21), 4, ALL, weigh=2, decay=1.0)

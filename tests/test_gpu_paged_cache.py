@@ -238,3 +238,46 @@ def test_a_run_of_all_of_them(e4m3):
     table.copy_(to)
     for news in ([1, 1], [5, 1], [1, 40]):
         step(news, 1, 1.0)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_the_cache_class(e4m3):
+    """Prompts in chunks, tokens, an eviction of one of two sequences, more tokens, a sequence that leaves and one that comes."""
+    Hq, Hkv, D, page = 8, 2, 64, 16
+    ks, vs = synth.e4m3_scales(Hkv, 4, device="cuda") if e4m3 else (None, None)
+    cache = u.PagedKVCache(2, Hkv, 64, page, 400, D, dtype=torch.uint8 if e4m3 else torch.bfloat16, k_scale=ks, v_scale=vs, weights=True)
+    g = torch.Generator().manual_seed(31)
+    values = lambda: tuple(wide(x, s) for x, s in ((cache.k, ks), (cache.v, vs)))
+
+    def step(n, weigh=0, **kw):
+        cache.extend(n)
+        q, kn, vn = (torch.randn(sum(n), H, D, generator=g).to(torch.bfloat16).cuda().transpose(0, 1) for H in (Hq, Hkv, Hkv))
+        cache.append(kn, vn)
+        out, lse = cache.attend(q, 4, ALL, weigh=weigh, **kw)
+        k, v = values()
+        o, l, _ = oracle.paged_attn(to_np(q), k, v, cache.pages, cache.rows, cache.cu.cpu().tolist(), 4, ALL)
+        assert out_ok(to_np(out), o) and max_abs(to_np(lse), l) <= TOL_LSE_BF16
+        for b, m in enumerate(n):  # the newest row is what was appended
+            if m and not e4m3:
+                r = cache.rows[b] - 1
+                assert torch.equal(cache.k[cache.pages[b][r // page], :, r % page], kn[:, sum(n[:b + 1]) - 1])
+
+    step([130, 60])
+    step([50, 1], weigh=16)
+    step([1, 1], weigh=1)
+    k, v = values()
+    before, _ = oracle.paged_rows(k, cache.pages[0], cache.rows[0])
+    w = np.stack([[float(cache.weight[cache.pages[0][j // page], h, j % page]) for j in range(cache.rows[0])] for h in range(Hkv)])
+    free = len(cache.free)
+    rows, kept = cache.evict([70, 1000], sinks=2, recent=8)
+    assert rows.cpu().tolist() == [70, 62] and cache.rows == [70, 62] and len(cache.free) == free + 12 - 5
+    assert kept[1, :, :62].cpu().tolist() == [list(range(62))] * Hkv
+    after, _ = oracle.paged_rows(values()[0], cache.pages[0], 70)
+    for h in range(Hkv):
+        sel = oracle.paged_select(w[h], 70, 2, 8)
+        assert kept[0, h, :70].cpu().tolist() == sel.tolist() and np.array_equal(after[h], before[h][sel])
+    step([1, 1], weigh=1)
+    step([3, 20], weigh=4, decay=0.5)
+    cache.release(0)
+    step([40, 1], weigh=1)
+    assert sorted(cache.free + [p for ps in cache.pages for p in ps]) == list(range(64))
