@@ -142,7 +142,7 @@ struct PagedParts {
     float* ml;   // [units][S][cols][2]
     float* acc;  // [units][S][cols][D]
     int S, want, cols;
-    int groups;  // chunk kernel: slices of a workgroup, which merges them itself; S counts workgroups
+    int groups;  // chunk kernel: parts of a slice, which its workgroup merges itself
 };
 
 // Scores of few columns in exponents of 2, -inf where a column does not see the entry: [B * Hkv][cols][pitch], pitch >= entries.

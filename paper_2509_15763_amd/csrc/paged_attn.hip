@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void paged_combine_chunk_kernel(PagedAttn a, P
     if (ncol <= min_cols || c0 < 0 || col >= ncol) return;
     const int pe = s.p0 + (min(c0 + kChunkCols, ncol) - 1) / G;
     const int E = pe >= 0 ? paged_walk(mask_shape(a.mask), max(s.p0 + c0 / G, 0), pe + 1).E : 0;
-    const int n = (paged_slices(E, parts.S * parts.groups, parts.want, 32).n + parts.groups - 1) / parts.groups;
+    const int n = paged_slices(E, parts.S, parts.want, 32).n;
     if (n <= 1) return;
     const size_t at0 = (((size_t)tile * Hkv + hk) * parts.S) * kChunkCols + (col - c0);
     const f32x2* ml = (const f32x2*)parts.ml + at0;
@@ -342,6 +342,31 @@ struct Plan {
     size_t bytes;
 };
 
+// How the walks of a launch's `busy` tiles are cut, the longest of E entries, avg in the mean: the split whose end comes first,
+// in steps of 32 entries (about 1 us at D = 128).  A CU has room for two workgroups of four waves or one of eight that takes a
+// slice in two halves; a step takes two workgroups 1.08, two halves 1.2 and a lone workgroup 1.0, starting and ending a workgroup about
+// 5, the merge of slices 8 and the time of the partial results' bytes.  us, by this / by as many slices as fill the CUs, in halves
+// up to 256 tiles (32/8 heads): 2048 tokens from the first 60 / 72, 512 at 32K 312 / 331, 64 at 1000 22.2 / 25.0, 64 at 32K 58.1 / 58.9;
+// 8/1 heads, 700 at 32K 127 / 138.
+struct ChunkSplit {
+    int groups, S;
+};
+ChunkSplit split_chunks(long busy, int E, double avg) {
+    ChunkSplit best = {1, 1};
+    double least = 1e30;
+    for (int g = 1; g <= 2; ++g)
+        for (int S = 1; S <= 32 && (S == 1 || E / S >= 256); ++S) {
+            const long wgs = busy * S, slots = g == 1 ? 512 : 256, rounds = (wgs + slots - 1) / slots;
+            const double steps = std::max((double)E, rounds * avg) / 32.0 / (S * g);
+            const double t = steps * (g == 2 ? 1.2 : wgs > 256 ? 1.08 : 1.0) + 5.0 * rounds + (S > 1 ? 8.0 + 0.026 * wgs : 0.0);
+            if (t < least) {
+                least = t;
+                best = {g, S};
+            }
+        }
+    return best;
+}
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 int built_for(int D) { return D <= 64 ? 64 : D <= 96 ? 96 : 128; }
@@ -377,14 +402,15 @@ Plan make_plan(const PagedAttn& a, char* ws) {
     }
     if (p.chunk) {
         p.ntiles = (int)((long)T * G / kChunkCols) + B;
-        const long units = (long)p.ntiles * Hkv, busy = (long)((long)T * G + kChunkCols - 1) / kChunkCols * Hkv;  // workgroups, those with work
+        const long units = (long)p.ntiles * Hkv, busy = (long)((long)T * G + kChunkCols - 1) / kChunkCols * Hkv;  // tiles, those with work
         const int rows = std::min(a.batch.max_new, kChunkCols / G + 1);
-        const int E = paged_walk(m, std::max(0, a.batch.max_kv - rows), a.batch.max_kv).E;
-        p.chk.groups = busy <= 256 ? 2 : 1;
-        int S = (int)std::min<long>(32, std::max<long>(1, 256 / busy));
-        S = std::max(1, std::min(S, (E + 511) / 512));
-        p.chk.S = S;
-        p.chk.want = S * p.chk.groups == 1 ? 1 << 24 : std::max(256, (E + S * p.chk.groups - 1) / (S * p.chk.groups));
+        const int E = paged_walk(m, std::max(0, a.batch.max_kv - rows), a.batch.max_kv).E;  // the last tile of the longest walk
+        const int first = std::max(0, a.batch.max_kv - a.batch.max_new);
+        const int E0 = paged_walk(m, first, std::min(first + rows, a.batch.max_kv)).E;        // and its sequence's first
+        const ChunkSplit x = split_chunks(busy, E, 0.5 * ((double)E + E0));
+        p.chk.groups = x.groups;
+        p.chk.S = x.S;
+        p.chk.want = x.S == 1 ? 1 << 24 : (E + x.S - 1) / x.S;
         place(p.chk, (size_t)units, kChunkCols);
     }
     if (p.few && a.weigh) {

@@ -59,11 +59,13 @@ __global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a
     const int pf = s.p0 + c0 / G, pe = s.p0 + c1 / G;
     PagedWalk walk = {0, 0, 0};
     if (pe >= 0) walk = paged_walk(m, max(pf, 0), pe + 1);
-    const PagedSlices sl = paged_slices(walk.E, parts.S * GROUPS, parts.want, BN);
-    if (slice * GROUPS >= sl.n) return;
-    const int e0 = min(walk.E, (slice * GROUPS + group) * sl.per), e1 = min(walk.E, e0 + sl.per);
-    const int nsteps = (e1 - e0 + BN - 1) / BN;  // the first group has no fewer than the second, and both meet at every step
-    const int nmeet = GROUPS > 1 ? (min(walk.E, (slice * GROUPS + 1) * sl.per) - slice * GROUPS * sl.per + BN - 1) / BN : nsteps;
+    const PagedSlices sl = paged_slices(walk.E, parts.S, parts.want, BN);
+    if (slice >= sl.n) return;
+    const int a0 = slice * sl.per, a1 = min(walk.E, a0 + sl.per);                   // the workgroup's entries
+    const int per = ((a1 - a0 + GROUPS - 1) / GROUPS + BN - 1) / BN * BN;          // of them a group's
+    const int e0 = min(a1, a0 + group * per), e1 = min(a1, e0 + per);
+    const int nsteps = (e1 - e0 + BN - 1) / BN;
+    const int nmeet = GROUPS > 1 ? (min(per, a1 - a0) + BN - 1) / BN : nsteps;     // both groups meet at every step of the first, which has no fewer
 
     // ---- the wave's columns
     const int cw = c0 + 32 * wv;  // first
@@ -362,7 +364,7 @@ __global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a
         const int col = cw + 16 * qb + r16;
         if (col > c1) continue;
         const float vmul = E4M3 ? a.kv.vscale[hk] : 1.f;
-        if (sl.n > GROUPS) {
+        if (sl.n > 1) {
             const size_t at_col = (((size_t)tile * Hkv + hk) * parts.S + slice) * kChunkCols + (col - c0);
             if (g4 == 0) *(f32x2*)(parts.ml + 2 * at_col) = f32x2{mr[qb] * c, lt};
 #pragma unroll
