@@ -162,6 +162,32 @@ def test_what_lies_outside_the_window_does_not_reach_it():
     assert torch.isnan(out[:, hit].float()).all()
 
 
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_values_that_are_not_finite_far_apart(e4m3, D):
+    # one element of V at both ends of the window, of gists left of it and of new rows: it reaches the rows that see it and no other
+    # element of them, however many steps of a walk, slices and sequences lie between
+    r, W, at, what = 4, 1500, 3, float("nan") if e4m3 else float("inf")
+    case = Paged([3000, 2000, 900], [700, 300, 900], 64, 4, 2, D, e4m3=e4m3, seed=21)
+    clean, clean_lse = run(case.cuda(), r, W)
+    seen = torch.zeros(case.T, dtype=torch.bool)
+    for b, (L, n) in enumerate(zip(case.lens, case.news)):
+        for j in (L - n - W + 8, L - n - W + 40, 4, L - 43, L - 3):
+            if j < 0 or (j == 4 and b != 1):
+                continue
+            case.v[int(case.table[b, j // 64]), :, j % 64, at] = 0x7F if e4m3 else what
+            for i in range(n):
+                p = L - n + i
+                seen[int(case.cu[b]) + i] |= j <= p and (p - j < W or (j + 1) % (r + 1) == 0)
+    assert 0 < int(seen.sum()) < case.T
+    out, lse = run(case.cuda(), r, W)
+    assert torch.equal(lse, clean_lse) or max_abs(to_np(lse), to_np(clean_lse)) <= 2 * TOL_LSE_BF16
+    got = out[..., at].float().cpu()
+    assert (torch.isnan(got) if e4m3 else got == what)[:, seen].all()
+    out[:, seen.to(out.device), at] = clean[:, seen.to(out.device), at]
+    assert max_abs(to_np(out), to_np(clean)) <= 2 * TOL_OUT_BF16
+
+
 @pytest.mark.parametrize("weigh,decay", [(1, 1.0), (3, 0.0), (100, 0.5), (1 << 30, 1.0)])
 @pytest.mark.parametrize("name", ["one key", "decode", "decode, odd page", "decode, group of 32", "decode, group of 48", "drafts", "drafts, D 64",
                                   "chunk", "chunk, group of 3, D 96", "chunk at the end", "mixed", "no new rows, no rows", "more new rows than rows"])
