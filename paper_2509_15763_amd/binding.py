@@ -1361,14 +1361,16 @@ class PagedKVCache:
         not cut all its rows."""
         if self.weight is None:
             raise UnigistError("evict needs a cache with weights=True")
-        keep = [min(int(x), r) for x, r in zip(keep, self.rows)]
+        keep = [int(x) for x in keep]
         if len(keep) != self.B or min(keep) < 0:
             raise UnigistError("evict takes a number of rows for each of the B sequences")
+        keep = [min(k, r) for k, r in zip(keep, self.rows)]
         cut = [k < r for k, r in zip(keep, self.rows)]
         per = [-(-k // self.page) if c else 0 for k, c in zip(keep, cut)]
         if sum(per) > len(self.free):
             raise UnigistError("out of pages")
-        fresh = [[self.free.pop() for _ in range(m)] for m in per]
+        free = list(self.free)  # kept if the call below refuses
+        fresh = [[free.pop() for _ in range(m)] for m in per]
         to = torch.full((self.B, max(max(per), 1)), -1, dtype=torch.int32)
         for b, p in enumerate(fresh):
             to[b, :len(p)] = torch.tensor(p, dtype=torch.int32)
@@ -1376,6 +1378,7 @@ class PagedKVCache:
         want = torch.tensor([k if c else 0 for k, c in zip(keep, cut)], dtype=torch.int32).to(self.k.device)
         rows, kept = paged_evict(self.k, self.v, self.table, self.kv_len, self.weight, want, self.k, self.v, to.to(self.k.device),
                                  max(max(self.rows), 1), max(max(keep), 1), sinks=sinks, recent=recent, weight_out=self.weight)
+        self.free = free
         for b, c in enumerate(cut):
             if c:
                 self.free.extend(self.pages[b])

@@ -46,3 +46,13 @@ def test_refusals_change_nothing():
         make(weights=False).evict([0, 0, 0])
     with pytest.raises(u.UnigistError):
         make(dtype=torch.uint8)  # no scales
+
+
+@pytest.mark.parametrize("keep", [[1, 1, 1, 1], [1, 1], [5, 2, 1]], ids=["too many", "too few", "refused by the call"])
+def test_an_eviction_that_is_refused_changes_nothing(keep):
+    c = make()  # on the CPU: the call itself refuses
+    c.extend([9, 4, 1])
+    before = (list(c.rows), [list(p) for p in c.pages], list(c.free), c.kv_len.tolist())
+    with pytest.raises(u.UnigistError):
+        c.evict(keep)
+    assert before == (c.rows, c.pages, c.free, c.kv_len.tolist())
