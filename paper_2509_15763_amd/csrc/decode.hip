@@ -87,15 +87,6 @@ template <int E> struct RowChunk<fp8_t, E> {
     }
 };
 
-// sum over the 16 lanes of a DPP row; every lane ends with the total
-__device__ __forceinline__ float row16_sum(float x) {
-    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, false));   // quad_perm [1,0,3,2]
-    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4E, 0xf, 0xf, false));   // quad_perm [2,3,0,1]
-    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x141, 0xf, 0xf, false));  // row_half_mirror
-    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x140, 0xf, 0xf, false));  // row_mirror
-    return x;
-}
-
 // workspace layout per (b, hq, split): [m, l, acc[D]] floats.
 // TQ: type of the queries; T: type the cache is stored in.  A cache of E4M3 codes comes with one scale per kv
 // head for K and for V (element = code * scale): the K scale is folded into the query, the V scale into the

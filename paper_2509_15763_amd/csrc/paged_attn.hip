@@ -289,9 +289,7 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(PagedAttn a, int mi
         for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float x = sum[half][kb][i];
-#pragma unroll
-                for (int off = 1; off < 16; off <<= 1) x += __shfl_xor(x, off, 64);
+                const float x = row16_sum(sum[half][kb][i]);
                 if (r16 == 4 * kb + i) own = x;
             }
         const int j = j0 + 64 * half + 16 * (r16 >> 2) + 4 * g4 + (r16 & 3);

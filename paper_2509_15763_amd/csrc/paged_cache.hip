@@ -51,12 +51,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedKv c, PagedBatch
 // left to take, lowest first, are numbered in row order.  Bound by latency: a thread holds the keys of PER rows, kSel apart, in
 // registers (all pages' numbers and then all weights in flight); sequences of more than PER * kSel rows are fetched again,
 // block by block, in each of the passes.  Rows are numbered from the counts of every 64 rows, scanned once.
-// 8 heads of 32768 rows 44.8 us with the keys in LDS, eight in flight and a wave numbering a stretch of rows; 64 x 8 of 2304 20.2.
+// 8 heads of 32768 rows 30 us (44.8 with the keys in LDS, eight in flight and a wave numbering a stretch of rows), 64 x 8 of 2304 16 (20.2).
 constexpr int kSel = 1024;  // threads
 constexpr int kBins = 4096;
 
 __device__ __forceinline__ unsigned weight_key(float w) {
-    if (w != w) return 0u;
+    if (w != w) return 1u;  // 0: rows past the end, which no pass has to tell apart then
     const unsigned u = __float_as_uint(w + 0.f);  // -0 as 0
     const unsigned m = (u >> 31) ? ~u : (u | 0x80000000u);
     return m < 0xfffffffeu ? m : 0xfffffffeu;
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kSel) void paged_select_kernel(PagedKv c, PagedKv t
 #pragma unroll
             for (int i = g; i < g + BATCH; ++i) {
                 const int j = base + i * kSel + tid;
-                key[i] = j < sinks || j >= len - recent ? 0xffffffffu : weight_key(__uint_as_float(key[i]));
+                key[i] = j >= len ? 0u : j < sinks || j >= len - recent ? 0xffffffffu : weight_key(__uint_as_float(key[i]));
             }
         }
     };
@@ -133,8 +133,10 @@ __global__ __launch_bounds__(kSel) void paged_select_kernel(PagedKv c, PagedKv t
             const int base = k * PER * kSel;
             if (nblocks > 1) fetch(base);
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (base + i * kSel + tid < len && (p == 0 || ((key[i] ^ limit) >> up) == 0u)) atomicAdd(&hist[(key[i] >> down) & (bins - 1)], 1);
+            for (int i = 0; i < PER; ++i) {
+                if (base + i * kSel >= len) break;
+                if (p == 0 || ((key[i] ^ limit) >> up) == 0u) atomicAdd(&hist[(key[i] >> down) & (bins - 1)], 1);
+            }
         }
         __syncthreads();
         // bins per thread from the top: thread 0 has the largest digits
@@ -168,22 +170,21 @@ __global__ __launch_bounds__(kSel) void paged_select_kernel(PagedKv c, PagedKv t
     }
     // ---- numbering
     int over0 = 0, ties0 = 0;  // of the blocks so far
-    const unsigned long long before = (1ull << lane) - 1ull;
 #pragma unroll 1
     for (int k = 0; k < nblocks; ++k) {
         const int base = k * PER * kSel;
         if (nblocks > 1) fetch(base);
-        for (int i = tid; i < kGroups; i += kSel) overs[i] = ties[i] = 0;
-        __syncthreads();
+        int no = 0, nt = 0;  // lane i: of the wave's i-th 64 rows
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (base + i * kSel >= len) break;
-            const bool in = base + i * kSel + tid < len;
-            const unsigned long long ob = __builtin_amdgcn_ballot_w64(in && key[i] > limit), tb = __builtin_amdgcn_ballot_w64(in && key[i] == limit);
-            if (lane == 0) {
-                overs[i * kWaves + wave] = __popcll(ob);
-                ties[i * kWaves + wave] = __popcll(tb);
-            }
+            const int o = __popcll(__builtin_amdgcn_ballot_w64(key[i] > limit)), t = __popcll(__builtin_amdgcn_ballot_w64(key[i] == limit));
+            no = lane == i ? o : no;
+            nt = lane == i ? t : nt;
+        }
+        if (lane < PER) {
+            overs[lane * kWaves + wave] = no;
+            ties[lane * kWaves + wave] = nt;
         }
         __syncthreads();
         if (wave < 2) {  // one wave scans each
@@ -204,13 +205,17 @@ __global__ __launch_bounds__(kSel) void paged_select_kernel(PagedKv c, PagedKv t
             if (lane == 63) sums[wave] = all;
         }
         __syncthreads();
+        const int at_o = over0 + overs[min(lane, PER - 1) * kWaves + wave], at_t = ties0 + ties[min(lane, PER - 1) * kWaves + wave];
+        auto in_front = [&](bool x, int from) __attribute__((always_inline)) {
+            const unsigned long long m = __builtin_amdgcn_ballot_w64(x);
+            return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, (unsigned)from));
+        };
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (base + i * kSel >= len) break;
             const int j = base + i * kSel + tid;
-            const bool is_over = j < len && key[i] > limit, is_tie = j < len && key[i] == limit;
-            const int o = over0 + overs[i * kWaves + wave] + __popcll(__builtin_amdgcn_ballot_w64(is_over) & before);
-            const int t = ties0 + ties[i * kWaves + wave] + __popcll(__builtin_amdgcn_ballot_w64(is_tie) & before);
+            const bool is_over = key[i] > limit, is_tie = key[i] == limit;  // limit > 0
+            const int o = in_front(is_over, __builtin_amdgcn_readlane(at_o, i)), t = in_front(is_tie, __builtin_amdgcn_readlane(at_t, i));
             if (is_over || (is_tie && t < left)) list[o + min(t, left)] = j;  // in front of it: o rows above the limit, t at it
         }
         over0 += sums[0];
