@@ -164,7 +164,7 @@ __global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a
 #pragma unroll
     for (int db = 0; db < DB; ++db) voff[db] = tr16_lane_off16<CH>(db);
 
-    // Masked tiles whose V holds numbers that are not finite are left for a second walk over the steps from the first of them to the
+    // Masked tiles whose V holds numbers that are not finite, or which miss a row's page, are left for a second walk over the steps from the first of them to the
     // last: their product is many times as long, and where the two meet in one step, every step copies its accumulators (4096
     // tokens at 28K: 2103 us with both in one step, 1955 us so).
     int c_first = 0x7fffffff, c_last = -1;
@@ -217,7 +217,9 @@ __global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a
 #pragma unroll
                 for (int e = 0; e < 4; ++e) odd |= not_finite2(x[e]);
             }
-            const bool careful = __builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0u) != 0ull;
+            // A row whose page is not there stands for one of another sequence, which may change between the walks.
+            const bool missing = (gone & bits_below(e1 - base)) != 0u;
+            const bool careful = missing || __builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0u) != 0ull;
             if (careful != CAREFUL) {
                 if (!CAREFUL) {
                     c_first = min(c_first, it);
