@@ -8,8 +8,8 @@
 //   bf16: direct global -> LDS loads; codes: through registers, widened once per workgroup on the way.
 // Places: 256 entries (eight steps) at a time, one per thread, into one of two tables in LDS; the table entries of the next
 // 256 are loaded a block ahead and the places of a step are read from LDS one step ahead.
-// Few workgroups: a lone wave per SIMD takes about 2000 cycles a step, two together 2200, so the entries of a tile are shared out
-// in slices, two to a workgroup of eight waves (GROUPS, merged through LDS), and from there on to workgroups (merged by
+// Few workgroups: a lone wave per SIMD took about 2000 cycles a step where two together took 2200 (now 1900), so the entries of a
+// tile are shared out in slices, two to a workgroup of eight waves (GROUPS, merged through LDS), and from there on to workgroups (merged by
 // paged_combine_chunk_kernel).
 #include "paged_common.h"
 
@@ -164,9 +164,9 @@ __global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a
 #pragma unroll
     for (int db = 0; db < DB; ++db) voff[db] = tr16_lane_off16<CH>(db);
 
-    // Masked tiles whose V holds numbers that are not finite, or which miss a row's page, are left for a second walk over the steps from the first of them to the
-    // last: their product is many times as long, and where the two meet in one step, every step copies its accumulators (4096
-    // tokens at 28K: 2103 us with both in one step, 1955 us so).
+    // Masked tiles whose V holds numbers that are not finite, or which miss a row's page, are left for a second walk over the steps
+    // from the first of them to the last: their product is many times as long, and where the two meet in one step, every step
+    // copies its accumulators (4096 tokens at 28K: 2103 us with both in one step, 1955 us so).
     int c_first = 0x7fffffff, c_last = -1;
     auto tile_step = [&](auto bufc, auto carefulc, int it, unsigned gone) __attribute__((always_inline)) {
         constexpr int BUF = decltype(bufc)::value;
