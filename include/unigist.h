@@ -540,7 +540,8 @@ size_t unigist_paged_attn_workspace(const unigist_paged_cache* cache, int B, int
  * Eviction by weight: of the kv_len[b] rows of sequence b, every kv head keeps keep[b] (all, if there are no more) and
  * copies them, in order, to the rows 0, 1, .. of sequence b in `dst`, with their weights where dst has them.  First in are
  * the protected rows, the first `sinks` and the last `recent`, then the others by weight, largest first (NaN below
- * every number); of equal ones the lower row.
+ * every number); of equal ones the lower row.  The rows of dst are numbered anew, for every kv head on its own: there row
+ * numbers are no positions, and unigist_paged_attn is to be called with a window that holds every row (W >= max_kv).
  * dst: the same pool under another table, or another pool (any page size; Hkv, D and dt of src); its pages are none of
  * those that src's tables name.  src is left as it is.
  * kv_len, keep: DEVICE, B ints, kv_len[b] <= max_kv, keep[b] <= max_keep.  kept (DEVICE [B, Hkv, max_keep], out): the rows

@@ -1272,7 +1272,8 @@ def paged_evict(k, v, table, kv_len, weight, keep, k_out, v_out, table_out, max_
     """Keep, for every kv head of every sequence, keep[b] (int32 [B] on the GPU) of its rows: the first `sinks`, the last
     `recent`, then those of most weight; they are copied in order to the rows 0, 1, .. under table_out in k_out, v_out (the
     same pool or another; pages that table does not name) -> rows kept, int32 [B] (-1: a sequence left alone), and
-    their old row numbers, int32 [B, Hkv, max_keep] (-1 past the end)."""
+    their old row numbers, int32 [B, Hkv, max_keep] (-1 past the end).  A row's new number is no position: attend to the kept
+    rows with a window that holds them all."""
     c = _paged_cache(k, v, table, None, None, weight, values=False)
     d = _paged_cache(k_out, v_out, table_out, None, None, weight_out, values=False)
     B = table.shape[0]
@@ -1296,6 +1297,10 @@ class PagedKVCache:
         cache.extend(n)                        # n[b] new rows for sequence b: pages, lengths, one copy to the GPU
         cache.append(k_new, v_new)             # [Hkv, T, D], T = sum(n)
         out, lse = cache.attend(q, r, W)       # [Hq, T, D]
+
+    A mask speaks of row numbers.  evict() numbers the rows that stay anew, differently for every kv head: from then on every
+    row of that sequence has to be inside the window (W >= its rows; the kept rows are the ones to attend to), and attend()
+    refuses a mask that would hide some of them.
     """
 
     def __init__(self, B, Hkv, n_pages, page, max_rows, D, dtype=torch.bfloat16, device="cuda", k_scale=None, v_scale=None,
@@ -1312,6 +1317,7 @@ class PagedKVCache:
         self.free = list(range(n_pages))
         self.pages, self.rows = [[] for _ in range(B)], [0] * B
         self.new = [0] * B   # rows added by the last extend
+        self.renumbered = [False] * B  # row numbers are no positions any more
         self._upload()
 
     def _upload(self):
@@ -1350,7 +1356,10 @@ class PagedKVCache:
                      weight=self.weight)
 
     def attend(self, q, r, W, sinks=0, window_mode=UNIGIST_WINDOW_SLIDING, weigh=0, decay=1.0, workspace=None):
-        """q [Hq, sum(n), D], the queries of those rows -> out, lse."""
+        """q [Hq, sum(n), D], the queries of those rows -> out, lse.  Of a sequence that was evicted from, r, W, sinks and
+        window_mode must show every row (W >= its rows, or as many sinks)."""
+        if any(m and x and max(int(W), int(sinks)) < n for m, x, n in zip(self.renumbered, self.new, self.rows)):
+            raise UnigistError("an evicted sequence's rows are renumbered: attend to all of them (W >= rows)")
         return paged_attn(q, self.k, self.v, self.table, self.kv_len, r, W, cu=self.cu, max_new=max(max(self.new), 1),
                           max_kv=max(max(self.rows), 1), sinks=sinks, window_mode=window_mode, k_scale=self.k_scale,
                           v_scale=self.v_scale, weight=self.weight, weigh=weigh, decay=decay, workspace=workspace)
@@ -1358,7 +1367,7 @@ class PagedKVCache:
     def evict(self, keep, sinks=0, recent=0):
         """Cut sequence b to keep[b] rows of each kv head (those with more), into new pages; the old ones become free.
         -> rows (int32 [B]) and their old numbers (int32 [B, Hkv, max(keep)]) on the GPU, as paged_evict; of a sequence that is
-        not cut all its rows."""
+        not cut all its rows.  The rows of a sequence that is cut are numbered anew (see above)."""
         if self.weight is None:
             raise UnigistError("evict needs a cache with weights=True")
         keep = [int(x) for x in keep]
@@ -1382,7 +1391,7 @@ class PagedKVCache:
         for b, c in enumerate(cut):
             if c:
                 self.free.extend(self.pages[b])
-                self.pages[b], self.rows[b] = fresh[b], keep[b]
+                self.pages[b], self.rows[b], self.renumbered[b] = fresh[b], keep[b], keep[b] > 0
             else:
                 rows[b] = keep[b]
                 kept[b, :, :keep[b]] = torch.arange(keep[b], dtype=torch.int32, device=kept.device)
@@ -1393,5 +1402,5 @@ class PagedKVCache:
     def release(self, b):
         """Sequence b is done: its pages become free, its place empty."""
         self.free.extend(self.pages[b])
-        self.pages[b], self.rows[b], self.new[b] = [], 0, 0
+        self.pages[b], self.rows[b], self.new[b], self.renumbered[b] = [], 0, 0, False
         self._upload()
