@@ -1365,7 +1365,9 @@ class PagedKVCache:
                           v_scale=self.v_scale, weight=self.weight, weigh=weigh, decay=decay, workspace=workspace)
 
     def evict(self, keep, sinks=0, recent=0):
-        """Cut sequence b to keep[b] rows of each kv head (those with more), into new pages; the old ones become free.
+        """Cut sequence b to keep[b] rows of each kv head (those with more), into free pages; its old ones become free.
+        Where there are too few for all of them, the smallest cuts come first and their old pages serve the next; where not even one
+        cut fits, it goes through a temporary copy into the sequence's own pages, so that a full pool can be cut too.
         -> rows (int32 [B]) and their old numbers (int32 [B, Hkv, max(keep)]) on the GPU, as paged_evict; of a sequence that is
         not cut all its rows.  The rows of a sequence that is cut are numbered anew (see above)."""
         if self.weight is None:
@@ -1373,31 +1375,75 @@ class PagedKVCache:
         keep = [int(x) for x in keep]
         if len(keep) != self.B or min(keep) < 0:
             raise UnigistError("evict takes a number of rows for each of the B sequences")
+        if int(sinks) < 0 or int(recent) < 0:
+            raise UnigistError("evict takes sinks and recent of at least 0")
         keep = [min(k, r) for k, r in zip(keep, self.rows)]
-        cut = [k < r for k, r in zip(keep, self.rows)]
-        per = [-(-k // self.page) if c else 0 for k, c in zip(keep, cut)]
-        if sum(per) > len(self.free):
-            raise UnigistError("out of pages")
-        free = list(self.free)  # kept if the call below refuses
-        fresh = [[free.pop() for _ in range(m)] for m in per]
-        to = torch.full((self.B, max(max(per), 1)), -1, dtype=torch.int32)
-        for b, p in enumerate(fresh):
-            to[b, :len(p)] = torch.tensor(p, dtype=torch.int32)
-        # a sequence that is not cut asks for no rows and stays where it is
-        want = torch.tensor([k if c else 0 for k, c in zip(keep, cut)], dtype=torch.int32).to(self.k.device)
-        rows, kept = paged_evict(self.k, self.v, self.table, self.kv_len, self.weight, want, self.k, self.v, to.to(self.k.device),
-                                 max(max(self.rows), 1), max(max(keep), 1), sinks=sinks, recent=recent, weight_out=self.weight)
-        self.free = free
-        for b, c in enumerate(cut):
-            if c:
-                self.free.extend(self.pages[b])
-                self.pages[b], self.rows[b], self.renumbered[b] = fresh[b], keep[b], keep[b] > 0
-            else:
-                rows[b] = keep[b]
-                kept[b, :, :keep[b]] = torch.arange(keep[b], dtype=torch.int32, device=kept.device)
+        need = [-(-k // self.page) for k in keep]
+        todo = sorted((b for b in range(self.B) if keep[b] < self.rows[b]), key=lambda b: need[b])
+        dev, most = self.k.device, max(max(keep), 1)
+        rows = torch.tensor(keep, dtype=torch.int32).to(dev)
+        number = torch.arange(most, dtype=torch.int32, device=dev)
+        kept = torch.where(number < rows[:, None], number, -1)[:, None].repeat(1, self.Hkv, 1)
+        cut = False
+        try:
+            while todo:
+                n = room = 0
+                while n < len(todo) and room + need[todo[n]] <= len(self.free):
+                    room += need[todo[n]]
+                    n += 1
+                now, todo = todo[:max(n, 1)], todo[max(n, 1):]
+                if n:
+                    fresh, at = [], len(self.free)
+                    for b in now:
+                        fresh.append(self.free[at - need[b]:at])
+                        at -= need[b]
+                    got = self._cut(now, keep, fresh, sinks, recent, most)
+                    del self.free[at:]
+                    for b, p in zip(now, fresh):
+                        self.free.extend(self.pages[b])
+                        self.pages[b] = p
+                else:
+                    b = now[0]
+                    got = self._cut_in_place(b, keep, need[b], sinks, recent, most)
+                    self.free.extend(self.pages[b][need[b]:])
+                    del self.pages[b][need[b]:]
+                cut = True
+                for b in now:
+                    self.rows[b], self.renumbered[b] = keep[b], keep[b] > 0
+                at = torch.tensor(now).to(dev)
+                for x, y in zip((rows, kept), got):
+                    x.index_copy_(0, at, y)
+        except Exception:  # a call that is refused changes nothing; one that fails later leaves the cuts that were made
+            if cut:
+                self.new = [0] * self.B
+                self._upload()
+            raise
         self.new = [0] * self.B
         self._upload()
         return rows, kept
+
+    def _cut(self, seqs, keep, pages, sinks, recent, most, pool=None):
+        """The sequences `seqs` cut into `pages` (a list for each) of the pool (k, v, weight; None: this one) -> paged_evict's results."""
+        n, cols, to = len(seqs), max(max(len(self.pages[b]) for b in seqs), 1), max(max(map(len, pages)), 1)
+        x = torch.full((n * (cols + to + 2),), -1, dtype=torch.int32)
+        table, table_out, kv_len, want = x.split((n * cols, n * to, n, n))
+        for i, b in enumerate(seqs):
+            table[i * cols:i * cols + len(self.pages[b])] = torch.tensor(self.pages[b], dtype=torch.int32)
+            table_out[i * to:i * to + len(pages[i])] = torch.tensor(pages[i], dtype=torch.int32)
+            kv_len[i], want[i] = self.rows[b], keep[b]
+        table, table_out, kv_len, want = x.to(self.k.device).split((n * cols, n * to, n, n))
+        k, v, weight = pool or (self.k, self.v, self.weight)
+        return paged_evict(self.k, self.v, table.view(n, cols), kv_len, self.weight, want, k, v, table_out.view(n, to),
+                           max(max(self.rows[b] for b in seqs), 1), most, sinks=sinks, recent=recent, weight_out=weight)
+
+    def _cut_in_place(self, b, keep, n, sinks, recent, most):
+        """Sequence b cut into the first n of its own pages: its rows move within them, so through a pool of n pages."""
+        pool = [torch.empty((n,) + x.shape[1:], dtype=x.dtype, device=x.device) for x in (self.k, self.v, self.weight)]
+        got = self._cut([b], keep, [list(range(n))], sinks, recent, most, pool)
+        x = torch.tensor(list(range(n)) + self.pages[b][:n] + [keep[b]], dtype=torch.int32).to(self.k.device)
+        paged_evict(pool[0], pool[1], x[:n].view(1, n), x[2 * n:], pool[2], x[2 * n:], self.k, self.v, x[n:2 * n].view(1, n), keep[b],
+                    keep[b], weight_out=self.weight)  # all of them, in order
+        return got
 
     def release(self, b):
         """Sequence b is done: its pages become free, its place empty."""

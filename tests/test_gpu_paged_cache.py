@@ -281,3 +281,38 @@ def test_the_cache_class(e4m3):
     cache.release(0)
     step([40, 1], weigh=1)
     assert sorted(cache.free + [p for ps in cache.pages for p in ps]) == list(range(64))
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("n_pages,keep", [(21, [90, 33, 20]), (21, [145, 99, 60]), (22, [60, 100, 16]), (40, [90, 33, 20])],
+                         ids=["full", "full, all pages needed again", "a cut's pages serve the next", "room"])
+def test_the_cache_class_evicts_from_a_full_pool(n_pages, keep, e4m3):
+    Hkv, D, page, rows = 2, 64, 16, [150, 100, 64]
+    ks, vs = synth.e4m3_scales(Hkv, 4, device="cuda") if e4m3 else (None, None)
+    cache = u.PagedKVCache(3, Hkv, n_pages, page, 200, D, dtype=torch.uint8 if e4m3 else torch.bfloat16, k_scale=ks, v_scale=vs, weights=True)
+    g = torch.Generator().manual_seed(33)
+    for n in ([150, 80, 64], [0, 20, 0]):
+        cache.extend(n)
+        kn, vn = (torch.randn(sum(n), Hkv, D, generator=g).to(torch.bfloat16).cuda().transpose(0, 1) for _ in range(2))
+        cache.append(kn, vn)
+    assert len(cache.free) == n_pages - 21
+    cache.weight.copy_(torch.randn(cache.weight.shape, generator=g).exp())
+    hold = lambda: [[oracle.paged_rows(x.cpu().numpy(), cache.pages[b], cache.rows[b])[0] for x in (cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.weight)]
+                    for b in range(3)]
+    before = hold()
+    got, kept = cache.evict(keep, sinks=2, recent=9)
+    assert got.cpu().tolist() == [min(k, r) for k, r in zip(keep, rows)] == cache.rows
+    for b, after in enumerate(hold()):
+        for h in range(Hkv):
+            sel = oracle.paged_select(before[b][2][h].astype(np.float64), cache.rows[b], 2, 9)
+            assert kept[b, h].cpu().tolist() == sel.tolist() + [-1] * (max(cache.rows) - cache.rows[b])
+            for x, y in zip(before[b], after):
+                assert np.array_equal(x[h][sel], y[h])
+    assert sorted(cache.free + [p for ps in cache.pages for p in ps]) == list(range(n_pages))
+    cache.extend([1, 1, 1])
+    q, kn, vn = (torch.randn(3, H, D, generator=g).to(torch.bfloat16).cuda().transpose(0, 1) for H in (8, Hkv, Hkv))
+    cache.append(kn, vn)
+    out, lse = cache.attend(q, 4, ALL)
+    k, v = (wide(x, s) for x, s in ((cache.k, ks), (cache.v, vs)))
+    o, l, _ = oracle.paged_attn(to_np(q), k, v, cache.pages, cache.rows, cache.cu.cpu().tolist(), 4, ALL)
+    assert out_ok(to_np(out), o) and max_abs(to_np(lse), l) <= TOL_LSE_BF16

@@ -74,3 +74,59 @@ def test_a_mask_that_hides_rows_of_an_evicted_sequence_is_refused(calls):
     c.evict([0, 10, 2])  # all of it
     c.extend([5, 1, 0])
     c.attend(queries(c), 4, 4)
+
+
+def fill(c, rows, seed):
+    """Rows of random values and weights for every sequence; -> what each holds."""
+    g = torch.Generator().manual_seed(seed)
+    c.extend(rows)
+    for x in (c.k, c.v, c.weight):
+        x.copy_(torch.randn(x.shape, generator=g))
+    return contents(c)
+
+
+def contents(c):
+    """Per sequence its rows of k, v and weight, [Hkv, rows, ..]."""
+    return [[oracle.paged_rows(x.double().numpy(), c.pages[b], c.rows[b])[0] for x in (c.k, c.v, c.weight[..., None])] for b in range(c.B)]
+
+
+@pytest.mark.parametrize("n_pages,rows,keep", [(10, [20, 20], [4, 4]),               # a full pool
+                                               (10, [20, 20], [17, 19]),             # all pages needed again
+                                               (11, [20, 20], [20, 8]),              # two pages needed, one free
+                                               (11, [20, 20], [7, 3]),               # the first cut's pages serve the second
+                                               (16, [20, 20, 19, 3], [16, 1, 19, 0]),
+                                               (30, [20, 20], [4, 4])])              # room for all
+def test_a_pool_without_room_for_what_stays_is_cut_all_the_same(calls, n_pages, rows, keep):
+    c = make(B=len(rows), n_pages=n_pages)
+    before = fill(c, rows, 1)
+    got, kept = c.evict(keep, sinks=1, recent=2)
+    stay = [min(k, r) for k, r in zip(keep, rows)]
+    assert c.rows == stay == got.tolist() and c.kv_len.tolist() == stay and c.new == [0] * len(rows)
+    assert kept.shape == (len(rows), c.Hkv, max(stay))
+    assert sorted(c.free + [p for ps in c.pages for p in ps]) == list(range(n_pages))
+    for b, after in enumerate(contents(c)):
+        assert len(c.pages[b]) == -(-stay[b] // c.page) and c.table[b, :len(c.pages[b])].tolist() == c.pages[b]
+        for h in range(c.Hkv):
+            want = list(range(rows[b])) if stay[b] == rows[b] else oracle.paged_select(before[b][2][h, :, 0], stay[b], 1, 2)
+            assert kept[b, h].tolist() == list(want) + [-1] * (max(stay) - stay[b])
+            for x, y in zip(before[b], after):
+                assert np.array_equal(x[h][want], y[h])
+
+
+def test_an_eviction_that_fails_halfway_leaves_whole_sequences(calls, monkeypatch):
+    c = make(B=2, n_pages=11)
+    before = fill(c, [20, 20], 2)
+    done = []
+
+    def second_fails(*a, **kw):
+        if done:
+            raise u.UnigistError("no memory, say")
+        done.append(1)
+        return evict(*a, **kw)
+
+    monkeypatch.setattr(u.binding, "paged_evict", second_fails)
+    with pytest.raises(u.UnigistError):
+        c.evict([7, 3])
+    assert c.rows == [20, 3] and c.kv_len.tolist() == [20, 3] and sorted(c.free + [p for ps in c.pages for p in ps]) == list(range(11))
+    for x, y in zip(before[0], contents(c)[0]):
+        assert np.array_equal(x, y)
