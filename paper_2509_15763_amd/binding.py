@@ -1350,14 +1350,20 @@ class PagedKVCache:
         self.new = n
         self._upload()
 
+    def _enough(self, what, t):
+        if t.dim() != 3 or t.shape[1] < sum(self.new):  # the library would count what is there as each sequence's last rows
+            raise UnigistError(f"{what} takes [H, {sum(self.new)}, D]: a row for each that extend() added")
+
     def append(self, k_new, v_new):
         """The rows that extend() made room for, [Hkv, sum(n), D] bf16."""
+        self._enough("append", k_new)
         paged_append(self.k, self.v, self.table, self.kv_len, k_new, v_new, cu=self.cu, k_scale=self.k_scale, v_scale=self.v_scale,
                      weight=self.weight)
 
     def attend(self, q, r, W, sinks=0, window_mode=UNIGIST_WINDOW_SLIDING, weigh=0, decay=1.0, workspace=None):
         """q [Hq, sum(n), D], the queries of those rows -> out, lse.  Of a sequence that was evicted from, r, W, sinks and
         window_mode must show every row (W >= its rows, or as many sinks)."""
+        self._enough("attend", q)
         if any(m and x and max(int(W), int(sinks)) < n for m, x, n in zip(self.renumbered, self.new, self.rows)):
             raise UnigistError("an evicted sequence's rows are renumbered: attend to all of them (W >= rows)")
         return paged_attn(q, self.k, self.v, self.table, self.kv_len, r, W, cu=self.cu, max_new=max(max(self.new), 1),

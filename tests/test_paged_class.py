@@ -130,3 +130,21 @@ def test_an_eviction_that_fails_halfway_leaves_whole_sequences(calls, monkeypatc
     assert c.rows == [20, 3] and c.kv_len.tolist() == [20, 3] and sorted(c.free + [p for ps in c.pages for p in ps]) == list(range(11))
     for x, y in zip(before[0], contents(c)[0]):
         assert np.array_equal(x, y)
+
+
+def test_too_few_rows_are_refused(calls):
+    # they would be written as, and attend as, the last rows of the sequences that the tensor still reaches
+    c = make()
+    c.extend([3, 0, 2])
+    for T in (0, 4):
+        x = torch.zeros(2, T, 8, dtype=torch.bfloat16)
+        with pytest.raises(u.UnigistError, match="row for each"):
+            c.append(x, x)
+        with pytest.raises(u.UnigistError, match="row for each"):
+            c.attend(x, 4, 100)
+    for T in (5, 8):  # rows behind the last sequence are left as they are
+        x = torch.zeros(2, T, 8, dtype=torch.bfloat16)
+        c.append(x, x)
+        c.attend(x, 4, 100)
+    with pytest.raises(u.UnigistError, match="row for each"):
+        c.attend(x[0], 4, 100)
