@@ -421,3 +421,21 @@ def test_hundreds_of_sequences():
         news.append((1, 1, 3, 40, 0, 9)[b % 6])
         lens.append(news[-1] + (b * 37) % 200)
     check(Paged(lens, news, 16, 4, 2, 64, seed=21), 4, ALL, weigh=2, decay=1.0)
+
+
+@pytest.mark.parametrize("lens,news", [([300, 77], [1, 1]), ([3000, 500], [1, 3]), ([5000, 900], [70, 1]), ([900, 400], [600, 300])],
+                         ids=["one slice", "slices", "sliced chunk", "chunks"])
+def test_results_in_place_of_the_queries(lens, news):
+    import ctypes as C
+    case = Paged(lens, news, 16, 8, 2, 128, seed=22)
+    c = case.cuda()
+    want, wl = run(c, 4, ALL)
+    cache = u.binding._paged_cache(c.k, c.v, c.table, None, None, None)
+    mask = (c.max_new, c.max_kv, 4, ALL, 0, 0)
+    need = u.unigist_paged_attn_workspace(C.byref(cache), 2, 8, c.T, *mask, 0)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    lse = torch.empty(8, c.T, device="cuda")
+    st = u.unigist_paged_attn(C.byref(cache), c.q.data_ptr(), c.q.data_ptr(), lse.data_ptr(), 2, 8, c.T, c.cu.data_ptr(), c.kv_len.data_ptr(), *mask, 128, 8 * 128,
+                              0, 1.0, ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert st == 0 and torch.equal(c.q.transpose(0, 1), want) and torch.equal(lse, wl)

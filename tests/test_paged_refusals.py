@@ -74,6 +74,16 @@ def test_attn_arguments(kw):
     assert attn(**kw) == EINVAL
 
 
+def test_results_on_the_queries_that_the_weights_read_again():
+    assert attn(q=FAKE, out=FAKE, weigh=1) == EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(q=None), dict(lse=None), dict(cu=None), dict(kv_len=None), dict(q=FAKE + 2), dict(hs=65), dict(rs=63), dict(rs=56), dict(hs=-64),
+                                dict(decay=-1.0), dict(decay=float("nan")), dict(decay=float("inf")), dict(ws=None), dict(ws=FAKE + 16), dict(ws_bytes=0)])
+def test_attn_arguments_with_results_apart_from_the_queries(kw):
+    assert attn(out=FAKE + 4096, **kw) == EINVAL
+
+
 def test_weights_asked_for_and_not_there():
     assert attn(cache(weight=None)) == EINVAL and size(cache(weight=None)) == 0
     assert size(cache(weight=None), weigh=0) > 0
