@@ -10,10 +10,11 @@ __device__ __forceinline__ float clamp448(float x) { return x != x ? x : fminf(f
 // Append.  A lane moves 8 elements (16 bytes of bf16), 16 lanes a row (those that a smaller head dimension has), K and V of
 // it.  Bound by the rows' bytes; for a token a sequence by latency.  Codes are RNE(clamp(x / scale, +-448)) with one correctly
 // rounded division, as unigist_quantize_e4m3 makes them.
+constexpr unsigned kAppendBlocks = 1u << 20;  // a row of the grid: a launch takes fewer than 2^32 threads an axis
 template <bool E4M3>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedKv c, PagedBatch x, const bf16_t* __restrict__ k_new,
                                                            const bf16_t* __restrict__ v_new, long long hs, int rs) {
-    const int row_id = blockIdx.x * 16 + threadIdx.x / 16, d = (threadIdx.x & 15) * 8;
+    const int row_id = (blockIdx.y * kAppendBlocks + blockIdx.x) * 16 + threadIdx.x / 16, d = (threadIdx.x & 15) * 8;
     const int t = row_id / c.Hkv, h = row_id - t * c.Hkv;
     if (t >= x.T || d >= c.D) return;
     const int b = seq_of_row(x, t);
@@ -244,8 +245,9 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedKv c, PagedKv to
 hipError_t launch_paged_append(const PagedKv& c, const PagedBatch& x, bool e4m3, const bf16_t* k_new, const bf16_t* v_new, long long hs,
                                int rs, hipStream_t st) {
     const unsigned blocks = (unsigned)(((long long)x.T * c.Hkv + 15) / 16);
-    if (e4m3) paged_append_kernel<true><<<dim3(blocks), 256, 0, st>>>(c, x, k_new, v_new, hs, rs);
-    else paged_append_kernel<false><<<dim3(blocks), 256, 0, st>>>(c, x, k_new, v_new, hs, rs);
+    const dim3 grid(blocks < kAppendBlocks ? blocks : kAppendBlocks, (blocks + kAppendBlocks - 1) / kAppendBlocks);
+    if (e4m3) paged_append_kernel<true><<<grid, 256, 0, st>>>(c, x, k_new, v_new, hs, rs);
+    else paged_append_kernel<false><<<grid, 256, 0, st>>>(c, x, k_new, v_new, hs, rs);
     return hipGetLastError();
 }
 

@@ -316,3 +316,21 @@ def test_the_cache_class_evicts_from_a_full_pool(n_pages, keep, e4m3):
     k, v = (wide(x, s) for x, s in ((cache.k, ks), (cache.v, vs)))
     o, l, _ = oracle.paged_attn(to_np(q), k, v, cache.pages, cache.rows, cache.cu.cpu().tolist(), 4, ALL)
     assert out_ok(to_np(out), o) and max_abs(to_np(lse), l) <= TOL_LSE_BF16
+
+
+def test_append_of_as_many_rows_as_four_billion_threads():
+    # 16 lanes a row: 2^28 rows are 2^32 threads, more than one axis of a launch takes
+    T, Hkv, D, page = 1 << 22, 64, 8, 4096
+    new = torch.randint(-32768, 32767, (Hkv, T, D), dtype=torch.int16, device="cuda").view(torch.bfloat16)
+    k, v = (torch.zeros(T // page, Hkv, page, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.arange(T // page, dtype=torch.int32, device="cuda").flip(0)[None].contiguous()
+    length, cu = torch.tensor([T], dtype=torch.int32, device="cuda"), torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    u.paged_append(k, v, table, length, new, new, cu=cu)
+    for x in (k, v):
+        for p in (0, 1, 77, T // page - 2, T // page - 1):
+            assert torch.equal(x[int(table[0, p])].view(torch.int16), new[:, p * page:(p + 1) * page].view(torch.int16))
+    assert torch.equal(k.view(torch.int16), v.view(torch.int16))
+    rows = torch.tensor([0, 1, T // 2, T - 1], device="cuda")
+    for h in range(Hkv):
+        at = table[0].long()[rows // page]
+        assert torch.equal(k[at, h, rows % page].view(torch.int16), new[h, rows].view(torch.int16))
