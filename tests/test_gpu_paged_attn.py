@@ -439,3 +439,11 @@ def test_results_in_place_of_the_queries(lens, news):
                               0, 1.0, ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
     torch.cuda.synchronize()
     assert st == 0 and torch.equal(c.q.transpose(0, 1), want) and torch.equal(lse, wl)
+
+
+def test_a_workspace_that_is_not_one_piece_of_memory_is_refused():
+    c = Paged([900, 500], [1, 1], 16, 8, 2, 128, seed=23).cuda()
+    for ws in (torch.empty(1, dtype=torch.uint8, device="cuda").expand(64 << 20), torch.empty(128 << 20, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(u.UnigistError):
+            run(c, 4, ALL, workspace=ws)
+    run(c, 4, ALL, workspace=torch.empty(16 << 20, dtype=torch.float32, device="cuda"))
