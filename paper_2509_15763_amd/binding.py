@@ -1258,6 +1258,7 @@ def paged_attn(q, k, v, table, kv_len, r, W, cu=None, max_new=None, max_kv=None,
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
         room = need
     else:
+        _dev(workspace)
         room = workspace.numel() * workspace.element_size()
     out = torch.empty_strided((Hq, T, D), (hs, rs, 1), dtype=torch.bfloat16, device=q.device)
     lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device)
