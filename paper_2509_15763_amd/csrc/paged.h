@@ -55,6 +55,12 @@ struct PagedSeq {
     int len;     // rows in use, the new ones among them
     int p0;      // position of its first new row (negative where len < n)
 };
+// how many new rows sequence b has
+__device__ __forceinline__ int paged_new(const PagedBatch& x, int b) {
+    if (!x.cu) return 1;
+    const int t0 = min(max(x.cu[b], 0), x.T);
+    return min(max(x.cu[b + 1], t0), x.T) - t0;
+}
 __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& x, int b) {
     PagedSeq s;
     s.t0 = x.cu ? min(max(x.cu[b], 0), x.T) : b;
@@ -143,6 +149,7 @@ struct PagedParts {
     float* acc;  // [units][S][cols][D]
     int S, want, cols;
     int groups;  // chunk kernel: parts of a slice, which its workgroup merges itself
+    int units;   // chunk kernel: tiles x slices of a kv head that there is room for; more tiles than that are not sliced
 };
 
 // Scores of few columns in exponents of 2, -inf where a column does not see the entry: [B * Hkv][cols][pitch], pitch >= entries.
@@ -167,6 +174,7 @@ struct PagedAttn {
     float decay;  // what was there is multiplied by this
 };
 
+// workspace; 0: more workgroups than a launch takes
 size_t paged_attn_bytes(const PagedAttn& a, bool e4m3);
 hipError_t launch_paged_attn(const PagedAttn& a, bool e4m3, void* ws, hipStream_t st);
 hipError_t launch_paged_append(const PagedKv& c, const PagedBatch& x, bool e4m3, const bf16_t* k_new, const bf16_t* v_new, long long hs,

@@ -108,7 +108,9 @@ extern "C" unigist_status unigist_paged_attn(const unigist_paged_cache* c, const
     if (q_head_stride % 8 != 0 || q_row_stride % 8 != 0 || q_row_stride < c->D || q_head_stride < 0) return UNIGIST_EINVAL;
     if (q_row_stride > 0x7fffffffLL) return UNIGIST_EUNSUPPORTED;
     const bool e4m3 = c->dt == UNIGIST_E4M3;
-    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < paged_attn_bytes(a, e4m3)) return UNIGIST_EINVAL;
+    const size_t need = paged_attn_bytes(a, e4m3);
+    if (need == 0) return UNIGIST_EUNSUPPORTED;
+    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need) return UNIGIST_EINVAL;
     a.q = (const bf16_t*)q;
     a.out = (bf16_t*)out;
     a.lse = lse;

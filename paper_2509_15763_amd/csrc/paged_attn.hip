@@ -6,7 +6,7 @@
 namespace unigist {
 
 hipError_t launch_paged_decode(const PagedAttn& a, bool e4m3, const PagedParts& parts, const PagedScores& scores, int cols, hipStream_t st);
-hipError_t launch_paged_chunk(const PagedAttn& a, bool e4m3, const PagedParts& parts, int ntiles, int min_cols, hipStream_t st);
+hipError_t launch_paged_chunk(const PagedAttn& a, bool e4m3, const PagedParts& parts, long long blocks, int min_cols, hipStream_t st);
 
 namespace {
 
@@ -91,15 +91,19 @@ __global__ __launch_bounds__(256) void paged_combine_chunk_kernel(PagedAttn a, P
     constexpr int C = (D + 63) / 64, NB = 8;
     const int sub = threadIdx.x & 15, hk = blockIdx.y, tile = blockIdx.x;
     const int Hkv = a.kv.Hkv, G = a.Hq / Hkv;
-    const int b = seq_of_tile(a.batch, G, tile);
+    const PagedTiles tiles = count_tiles(a.batch, G, min_cols);
+    const int S = slices_of(parts, tiles.total);
+    if (S <= 1 || tile >= tiles.total) return;
+    int nth;
+    const int b = seq_of_tile(a.batch, G, min_cols, tiles, tile, nth);
     const PagedSeq s = paged_seq(a.batch, b);
-    const int ncol = s.n * G, c0 = (tile - first_tile(s.t0, G, b)) * kChunkCols, col = c0 + blockIdx.z * 16 + (threadIdx.x >> 4);
-    if (ncol <= min_cols || c0 < 0 || col >= ncol) return;
+    const int ncol = s.n * G, c0 = nth * kChunkCols, col = c0 + blockIdx.z * 16 + (threadIdx.x >> 4);
+    if ((unsigned)nth * kChunkCols >= (unsigned)ncol || col >= ncol) return;
     const int pe = s.p0 + (min(c0 + kChunkCols, ncol) - 1) / G;
     const int E = pe >= 0 ? paged_walk(mask_shape(a.mask), max(s.p0 + c0 / G, 0), pe + 1).E : 0;
-    const int n = paged_slices(E, parts.S, parts.want, 32).n;
+    const int n = paged_slices(E, S, parts.want, 32).n;
     if (n <= 1) return;
-    const size_t at0 = (((size_t)tile * Hkv + hk) * parts.S) * kChunkCols + (col - c0);
+    const size_t at0 = (((size_t)tile * Hkv + hk) * S) * kChunkCols + (col - c0);
     const f32x2* ml = (const f32x2*)parts.ml + at0;
     f32x4 acc[C], x[NB][C];
     f32x2 y[NB];
@@ -325,15 +329,23 @@ __global__ __launch_bounds__(256) void paged_weigh_few_kernel(PagedAttn a, Paged
 
 // ---------------------------------------------------------------------------------------------
 // The launch: sequences of few columns (new rows x heads of a group) go to the decode kernel, the others to the chunk
-// kernel; a batch that may hold both launches both, and each leaves the other's sequences.
+// kernel; a batch that may hold both launches both, and each leaves the other's sequences.  The chunk kernel's workgroups are numbered
+// over the tiles that there are.
 // Scores of few columns are kept for the weights, 4 bytes a column and key for the 128 to 256 that reading K again takes, up to
 // this much memory.
 constexpr int kOneSlice = 384, kLongSlice = 2048;
 constexpr size_t kMostScores = (size_t)1 << 30;
+// Partial results of the decode kernel's slices: at most this much.  S slices of the longest sequence are kept for every one (4.3 GB
+// for 1024 sequences of up to 128K rows, 8 kv heads); so many sequences fill the CUs with longer slices too.
+constexpr size_t kMostParts = (size_t)1 << 30;
+// Partial results of the chunk kernel: for twice the tiles that the batch has if every sequence has new rows and one of them the chunk,
+// and for as many as this holds.  A batch of more tiles is cut in fewer slices each, which fill the CUs as well.
+constexpr size_t kChunkParts = (size_t)64 << 20;
 struct Plan {
     int few;      // columns that the decode kernel takes at most (0: not launched)
     bool chunk;   // is the chunk kernel launched?
-    int ntiles;
+    int ntiles;   // of a kv head at most
+    long long blocks;  // workgroups of the chunk kernel
     PagedParts dec, chk;
     PagedScores scores;  // x null: not kept
     bool keep_scores;
@@ -379,10 +391,10 @@ Plan make_plan(const PagedAttn& a, char* ws) {
     p.chunk = most > p.few;
     if (B == 1 && p.chunk) p.few = 0;
     size_t off = 0;
-    auto place = [&](PagedParts& x, size_t units, int cols) {
+    auto place = [&](PagedParts& x, size_t slices, int cols) {  // slices: of all units
         x.cols = cols;
         if (x.S <= 1) return;
-        const size_t n = units * x.S * cols;
+        const size_t n = slices * cols;
         x.ml = (float*)(ws + off);
         off += align256(n * 2 * sizeof(float));
         x.acc = (float*)(ws + off);
@@ -393,14 +405,16 @@ Plan make_plan(const PagedAttn& a, char* ws) {
         const long units = (long)B * Hkv;
         int want = (int)std::min<long>(((long)E * units + 255) / 256, kLongSlice);
         want = std::max(want, E <= kOneSlice ? E : 128);
-        want = std::max(want, (E + 63) / 64);
+        const size_t one = (size_t)units * std::min<long>(p.few, most) * (D + 2) * sizeof(float);  // a slice of each
+        const int most_slices = (int)std::max<size_t>(1, std::min<size_t>(64, kMostParts / one));  // the merge takes 64
+        want = std::max(want, (E + most_slices - 1) / most_slices);
         p.dec.want = (want + 127) / 128 * 128;
         p.dec.S = std::min(64, std::max(1, (E + p.dec.want - 1) / p.dec.want));
-        place(p.dec, (size_t)B * Hkv, (int)std::min<long>(p.few, most));
+        place(p.dec, (size_t)units * p.dec.S, (int)std::min<long>(p.few, most));
     }
     if (p.chunk) {
-        p.ntiles = (int)((long)T * G / kChunkCols) + B;
-        const long units = (long)p.ntiles * Hkv, busy = (long)((long)T * G + kChunkCols - 1) / kChunkCols * Hkv;  // tiles, those with work
+        const long cols = (long)T * G, busy = (cols + kChunkCols - 1) / kChunkCols * Hkv;  // tiles of all heads
+        p.ntiles = (int)(cols / kChunkCols + std::min<long>(B, cols / (p.few + 1)));          // a sequence that has any is of more than `few` columns
         const int rows = std::min(a.batch.max_new, kChunkCols / G + 1);
         const int E = paged_walk(m, std::max(0, a.batch.max_kv - rows), a.batch.max_kv).E;  // the last tile of the longest walk
         const int first = std::max(0, a.batch.max_kv - a.batch.max_new);
@@ -409,7 +423,11 @@ Plan make_plan(const PagedAttn& a, char* ws) {
         p.chk.groups = x.groups;
         p.chk.S = x.S;
         p.chk.want = x.S == 1 ? 1 << 24 : (E + x.S - 1) / x.S;
-        place(p.chk, (size_t)units, kChunkCols);
+        const long chunk = std::max<long>(T - B + 1, std::min(a.batch.max_new, T)) * G;  // columns of the chunk if the others are tokens
+        const long room = std::max<long>(2 * (chunk / kChunkCols + 1) * x.S, kChunkParts / ((size_t)Hkv * kChunkCols * (D + 2) * sizeof(float)));
+        p.chk.units = x.S == 1 ? p.ntiles : (int)std::min<long>(room, (long)p.ntiles * x.S);
+        p.blocks = (long long)std::max(p.chk.units, p.ntiles) * Hkv;
+        place(p.chk, (size_t)p.chk.units * Hkv, kChunkCols);
     }
     if (p.few && a.weigh) {
         p.scores.cols = p.dec.cols;
@@ -421,7 +439,8 @@ Plan make_plan(const PagedAttn& a, char* ws) {
             off += align256(n);
         }
     }
-    p.bytes = std::max<size_t>(off, 256);
+    // an axis of a launch takes fewer than 2^32 threads
+    p.bytes = p.blocks * 256 * std::max(p.chk.groups, 1) > 0xffffffffLL ? 0 : std::max<size_t>(off, 256);
     return p;
 }
 
@@ -433,7 +452,7 @@ hipError_t launch_combine(const PagedAttn& a, const Plan& p, hipStream_t st) {
         else paged_combine_kernel<D, 1><<<dim3((cols + 3) / 4, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, p.dec);
     }
     if (p.chunk && p.chk.S > 1)
-        paged_combine_chunk_kernel<D><<<dim3(p.ntiles, a.kv.Hkv, kChunkCols / 16), 256, 0, st>>>(a, p.chk, p.few);
+        paged_combine_chunk_kernel<D><<<dim3(std::min(p.ntiles, p.chk.units / 2), a.kv.Hkv, kChunkCols / 16), 256, 0, st>>>(a, p.chk, p.few);
     return hipGetLastError();
 }
 
@@ -444,7 +463,7 @@ size_t paged_attn_bytes(const PagedAttn& a, bool) { return make_plan(a, nullptr)
 hipError_t launch_paged_attn(const PagedAttn& a, bool e4m3, void* ws, hipStream_t st) {
     const Plan p = make_plan(a, (char*)ws);
     hipError_t e = hipSuccess;
-    if (p.chunk) e = launch_paged_chunk(a, e4m3, p.chk, p.ntiles, p.few, st);
+    if (p.chunk) e = launch_paged_chunk(a, e4m3, p.chk, p.blocks, p.few, st);
     if (e == hipSuccess && p.few) e = launch_paged_decode(a, e4m3, p.dec, p.keep_scores ? p.scores : PagedScores{}, p.few, st);
     const int D = built_for(a.kv.D);
     if (e == hipSuccess) e = D == 64 ? launch_combine<64>(a, p, st) : D == 96 ? launch_combine<96>(a, p, st) : launch_combine<128>(a, p, st);

@@ -32,7 +32,7 @@ struct ChunkSmem {
 };
 
 template <int D, bool E4M3, int GROUPS>
-__global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a, PagedParts parts, int ntiles, int min_cols) {
+__global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a, PagedParts parts, int min_cols) {
     constexpr int KS = D / 32, DB = D / 16, CH = D <= 64 ? 8 : 16;
     constexpr int RPI = 64 / CH;       // tile rows of one direct load
     constexpr int IPW = BN / RPI / 4;  // direct loads per wave, matrix and tile
@@ -49,17 +49,20 @@ __global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a
 
     // ---- which kv head, slice and tile: late tiles, which walk further, first
     const int hk = blockIdx.x % Hkv, rest = blockIdx.x / Hkv;
-    const int slice = rest % parts.S, tile = ntiles - 1 - rest / parts.S;
-    const int b = seq_of_tile(a.batch, G, tile);
+    const PagedTiles tiles = count_tiles(a.batch, G, min_cols);
+    const int S = slices_of(parts, tiles.total), slice = rest % S, tile = tiles.total - 1 - rest / S;
+    if (tile < 0) return;
+    int nth;
+    const int b = seq_of_tile(a.batch, G, min_cols, tiles, tile, nth);
     const PagedSeq s = paged_seq(a.batch, b);
-    const int ncol = s.n * G, c0 = (tile - first_tile(s.t0, G, b)) * kChunkCols;
-    if (ncol <= min_cols || c0 < 0 || c0 >= ncol) return;
+    const int ncol = s.n * G, c0 = nth * kChunkCols;
+    if ((unsigned)nth * kChunkCols >= (unsigned)ncol) return;  // boundaries that decrease
     const AttnShape m = mask_shape(a.mask);
     const int c1 = min(c0 + kChunkCols, ncol) - 1;  // last column
     const int pf = s.p0 + c0 / G, pe = s.p0 + c1 / G;
     PagedWalk walk = {0, 0, 0};
     if (pe >= 0) walk = paged_walk(m, max(pf, 0), pe + 1);
-    const PagedSlices sl = paged_slices(walk.E, parts.S, parts.want, BN);
+    const PagedSlices sl = paged_slices(walk.E, S, parts.want, BN);
     if (slice >= sl.n) return;
     const int a0 = slice * sl.per, a1 = min(walk.E, a0 + sl.per);                   // the workgroup's entries
     const int per = ((a1 - a0 + GROUPS - 1) / GROUPS + BN - 1) / BN * BN;          // of them a group's
@@ -399,7 +402,7 @@ __global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a
         if (col > c1) continue;
         const float vmul = E4M3 ? a.kv.vscale[hk] : 1.f;
         if (sl.n > 1) {
-            const size_t at_col = (((size_t)tile * Hkv + hk) * parts.S + slice) * kChunkCols + (col - c0);
+            const size_t at_col = (((size_t)tile * Hkv + hk) * S + slice) * kChunkCols + (col - c0);
             if (g4 == 0) *(f32x2*)(parts.ml + 2 * at_col) = f32x2{mr[qb] * c, lt};
 #pragma unroll
             for (int db = 0; db < DB; ++db) *(f32x4*)(parts.acc + at_col * D + 16 * db + 4 * g4) = o[db][qb] * vmul;
@@ -422,10 +425,8 @@ __global__ __launch_bounds__(NT * GROUPS, 2) void paged_chunk_kernel(PagedAttn a
 
 }  // namespace
 
-hipError_t launch_paged_chunk(const PagedAttn& a, bool e4m3, const PagedParts& parts, int ntiles, int min_cols, hipStream_t st) {
-    const long long blocks = (long long)ntiles * a.kv.Hkv * parts.S;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    auto go = [&](auto kern) { kern<<<dim3((unsigned)blocks), NT * parts.groups, 0, st>>>(a, parts, ntiles, min_cols); };
+hipError_t launch_paged_chunk(const PagedAttn& a, bool e4m3, const PagedParts& parts, long long blocks, int min_cols, hipStream_t st) {
+    auto go = [&](auto kern) { kern<<<dim3((unsigned)blocks), NT * parts.groups, 0, st>>>(a, parts, min_cols); };
     auto pick = [&](auto d) {
         constexpr int D = decltype(d)::value;
         if (parts.groups == 1) e4m3 ? go(paged_chunk_kernel<D, true, 1>) : go(paged_chunk_kernel<D, false, 1>);

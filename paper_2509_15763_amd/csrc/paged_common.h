@@ -8,21 +8,63 @@ namespace unigist {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kChunkCols = 128;  // (row, head) columns of a workgroup of the chunk kernel
 
-// Tiles of kChunkCols columns are numbered from floor(t0 * G / kChunkCols) + b on for sequence b, whose first new row is t0: that
-// leaves room for the ceil(n * G / kChunkCols) that it has.
-__device__ __forceinline__ int first_tile(int t0, int G, int b) { return (int)((unsigned)(t0 * G) / kChunkCols) + b; }
-// the sequence that a tile belongs to: the last one whose numbers begin at or below it; 64 sequences a step
-__device__ __forceinline__ int seq_of_tile(const PagedBatch& x, int G, int tile) {
-    const int lane = threadIdx.x & 63;
-    int n = 0;
-    for (int b0 = 0; b0 < x.B; b0 += 64) {
-        const int b = b0 + lane;
-        const bool below = b < x.B && first_tile(x.cu ? min(max(x.cu[b], 0), x.T) : b, G, b) <= tile;
-        const unsigned long long bits = __builtin_amdgcn_ballot_w64(below);
-        n += __popcll(bits);
-        if (~bits != 0ull) break;
+// The chunk kernel's tiles, of kChunkCols columns each: those of sequence 0, then of sequence 1, .. for sequences of more than
+// min_cols columns; the others have none.  Every wave counts them for itself, a lane the sequences lane * per .. of them, so that
+// launch and workspace go by the work of a batch and not by its number of sequences.
+struct PagedTiles {
+    int total;
+    int per, upto, own;  // per lane: sequences of a lane, tiles up to and with them, tiles of them
+};
+__device__ __forceinline__ int tiles_of(const PagedBatch& x, int G, int min_cols, int b) {
+    const int ncol = b < x.B ? paged_new(x, b) * G : 0;
+    return ncol > min_cols ? (ncol + kChunkCols - 1) / kChunkCols : 0;
+}
+__device__ __forceinline__ int scan64(int own) {  // sum of the lanes up to and with this one
+    int sum = own;
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8: rows of 16 lanes
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x112, 0xf, 0xf, false);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x114, 0xf, 0xf, false);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x118, 0xf, 0xf, false);
+    const int row = (threadIdx.x & 63) >> 4;
+    const int r0 = __builtin_amdgcn_readlane(sum, 15), r1 = r0 + __builtin_amdgcn_readlane(sum, 31), r2 = r1 + __builtin_amdgcn_readlane(sum, 47);
+    return sum + (row == 0 ? 0 : row == 1 ? r0 : row == 2 ? r1 : r2);
+}
+__device__ __forceinline__ PagedTiles count_tiles(const PagedBatch& x, int G, int min_cols) {
+    PagedTiles t;
+    t.per = (x.B + 63) / 64;
+    t.own = 0;
+    if (x.B == 1) {
+        t.total = t.upto = t.own = __builtin_amdgcn_readfirstlane(tiles_of(x, G, min_cols, 0));
+        return t;
     }
-    return max(n - 1, 0);
+    const int b0 = (int)(threadIdx.x & 63) * t.per;
+    for (int i = 0; i < t.per; ++i) t.own += tiles_of(x, G, min_cols, b0 + i);
+    t.upto = scan64(t.own);
+    t.total = __builtin_amdgcn_readlane(t.upto, 63);
+    return t;
+}
+// The sequence of tile 0 <= tile < total, and which of its tiles it is.
+__device__ __forceinline__ int seq_of_tile(const PagedBatch& x, int G, int min_cols, const PagedTiles& t, int tile, int& j) {
+    j = tile;
+    if (x.B == 1) return 0;
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(t.upto > tile));
+    j -= __builtin_amdgcn_readlane(t.upto - t.own, at);
+    if (t.per == 1) return at;
+    for (int b0 = at * t.per; b0 < x.B; b0 += 64) {  // among the lane's sequences, 64 at a time; tile lies in one of them
+        const int b = b0 + (int)(threadIdx.x & 63), own = b < (at + 1) * t.per ? tiles_of(x, G, min_cols, b) : 0, upto = scan64(own);
+        const unsigned long long behind = __builtin_amdgcn_ballot_w64(upto > j);
+        if (behind != 0ull) {
+            const int l = __builtin_ctzll(behind);
+            j -= __builtin_amdgcn_readlane(upto - own, l);
+            return b0 + l;
+        }
+        j -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return 0;  // boundaries that decrease
+}
+// Slices of a tile: as many as there is room for, at most S.
+__device__ __forceinline__ int slices_of(const PagedParts& parts, int total) {
+    return parts.S == 1 || (long long)total * parts.S <= parts.units ? parts.S : max(1, parts.units / total);
 }
 
 __device__ __forceinline__ unsigned bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }

@@ -447,3 +447,34 @@ def test_a_workspace_that_is_not_one_piece_of_memory_is_refused():
         with pytest.raises(u.UnigistError):
             run(c, 4, ALL, workspace=ws)
     run(c, 4, ALL, workspace=torch.empty(16 << 20, dtype=torch.float32, device="cuda"))
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_more_tiles_than_the_partial_results_have_room_for(e4m3):
+    # 40 drafts that the chunk kernel takes (20 columns) beside a chunk: 42 tiles of each of 8 kv heads where there is room for 126 slices,
+    # less than the five of every tile that one chunk would be cut in
+    news = [5] * 20 + [33] + [5] * 20 + [1] * 3
+    lens = [400 + 17 * b for b in range(20)] + [2500] + [1800 - 31 * b for b in range(20)] + [2000, 1, 300]
+    check(Paged(lens, news, 64, 32, 8, 128, e4m3=e4m3, seed=24), 4, ALL)
+
+
+@pytest.mark.parametrize("B", [300, 5000])
+def test_tiles_of_thousands_of_sequences(B):
+    # several sequences a lane, more than 64 of them; most without tiles, some at the ends of a lane's range
+    lens, news = [], []
+    for b in range(B):
+        news.append({0: 1, 1: 0, 2: 1, 3: 0, 4: 5, 78: 40, 79: 33, 80: 70}.get(b % 97, 0) if b else 40)
+        lens.append(news[-1] + (b * 37) % (200 if B < 1000 else 20))
+    news[-1], lens[-1] = 35, 60
+    check(Paged(lens, news, 16, 4, 1, 64, seed=25), 4, ALL)
+
+
+def test_one_row_a_sequence_with_a_group_of_many_heads():
+    # more columns than the decode kernel takes, without boundaries
+    case = Paged([300, 90, 700], [1, 1, 1], 16, 80, 2, 64, seed=26)
+    c = case.cuda()
+    want, wl = run(c, 4, ALL)
+    out, lse = u.paged_attn(c.q.transpose(0, 1), c.k, c.v, c.table, c.kv_len, 4, ALL)
+    wo, ll, _ = case.want(4, ALL)
+    for x, y in ((out, lse), (want, wl)):
+        assert out_ok(to_np(x), wo) and max_abs(to_np(y), ll) <= TOL_LSE_BF16

@@ -129,3 +129,22 @@ def test_bindings_refuse_tensors_that_are_not_on_the_gpu():
         u.paged_attn(q, k.float(), k.float(), t, n, 4, 8)
     with pytest.raises(u.UnigistError):
         u.paged_attn(q, k.byte(), k.byte(), t, n, 4, 8)  # codes without scales
+
+
+@pytest.mark.parametrize("B,T,max_new,max_kv", [(64, 95, 32, 32000), (256, 767, 512, 32768), (1024, 1087, 64, 16384), (1024, 1032, 9, 131072), (64, 64, 64, 12000),
+                                                (65535, 65635, 100, 1 << 23)])
+def test_the_workspace_goes_by_the_new_rows_and_not_by_the_sequences(B, T, max_new, max_kv):
+    # one chunk among tokens: partial results of the tokens' slices (1 GiB at most) and of what one chunk takes alone, not of a tile a sequence
+    c = cache(n_pages=1 << 15, page=64, Hkv=8, D=128)
+    kw = dict(Hq=32, max_new=max_new, max_kv=max_kv, W=1 << 23, weigh=0)
+    alone = size(c, B=1, T=max_new, **kw)
+    tokens = size(c, B=B, T=B, **dict(kw, max_new=1))
+    # 16 columns for the tokens where there is a chunk, 4 else; twice the chunk's tiles, and 64 MiB
+    assert size(c, B=B, T=T, **kw) <= min(4 * tokens, 1 << 30) + 3 * alone + (80 << 20)
+
+
+def test_more_workgroups_than_a_launch_takes():
+    # 2^24 workgroups of 256 threads of the chunk kernel
+    c = cache(n_pages=1 << 15, page=16, Hkv=51, D=8)
+    assert size(c, B=65535, Hq=255, T=1 << 23, max_new=1 << 23, max_kv=1 << 23, weigh=0) == 0
+    assert attn(c, B=65535, Hq=255, T=1 << 23, max_new=1 << 23, max_kv=1 << 23, weigh=0, hs=8, rs=8 * 255, out=FAKE + 4096) == EUNSUPPORTED
