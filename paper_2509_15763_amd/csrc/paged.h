@@ -153,9 +153,10 @@ struct PagedParts {
 };
 
 // Scores of few columns in exponents of 2, -inf where a column does not see the entry: [B * Hkv][cols][pitch], pitch >= entries.
+// Kept are those of the new rows whose attention counts, of sequences of at most `most` columns.
 struct PagedScores {
     float* x;
-    int cols;
+    int cols, most;
     int pitch;
 };
 

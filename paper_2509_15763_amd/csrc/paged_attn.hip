@@ -308,7 +308,7 @@ __global__ __launch_bounds__(256) void paged_weigh_few_kernel(PagedAttn a, Paged
     const int G = a.Hq / a.kv.Hkv;
     const PagedSeq s = paged_seq(a.batch, b);
     const int ncol = s.n * G;
-    if (ncol == 0 || ncol > scores.cols || j >= s.len) return;
+    if (ncol == 0 || ncol > scores.most || j >= s.len) return;
     const int at = pool_row(a.kv, b, hk, j);
     if (at < 0) return;
     const AttnShape m = mask_shape(a.mask);
@@ -317,10 +317,11 @@ __global__ __launch_bounds__(256) void paged_weigh_few_kernel(PagedAttn a, Paged
     float sum = 0.f;
     if (e >= 0) {
         const float* x = scores.x + ((size_t)b * a.kv.Hkv + hk) * scores.cols * scores.pitch + e;
-        for (int i = max(0, s.n - a.weigh); i < s.n; ++i)
+        const int i0 = max(0, s.n - a.weigh);
+        for (int i = i0; i < s.n; ++i)
             for (int g = 0; g < G; ++g) {
                 const float lse = a.lse[(size_t)(hk * G + g) * a.batch.T + s.t0 + i];
-                const float y = x[(size_t)(i * G + g) * scores.pitch];
+                const float y = x[(size_t)((i - i0) * G + g) * scores.pitch];
                 if (lse != -INFINITY && y != -INFINITY) sum += __builtin_amdgcn_exp2f(fmaf(-lse, kLog2e, y));
             }
     }
@@ -331,8 +332,8 @@ __global__ __launch_bounds__(256) void paged_weigh_few_kernel(PagedAttn a, Paged
 // The launch: sequences of few columns (new rows x heads of a group) go to the decode kernel, the others to the chunk
 // kernel; a batch that may hold both launches both, and each leaves the other's sequences.  The chunk kernel's workgroups are numbered
 // over the tiles that there are.
-// Scores of few columns are kept for the weights, 4 bytes a column and key for the 128 to 256 that reading K again takes, up to
-// this much memory.
+// Scores of few columns are kept for the weights, 4 bytes a key and column that counts for the 128 to 256 that reading K again takes, up
+// to this much memory.
 constexpr int kOneSlice = 384, kLongSlice = 2048;
 constexpr size_t kMostScores = (size_t)1 << 30;
 // Partial results of the decode kernel's slices: at most this much.  S slices of the longest sequence are kept for every one (4.3 GB
@@ -430,7 +431,8 @@ Plan make_plan(const PagedAttn& a, char* ws) {
         place(p.chk, (size_t)p.chk.units * Hkv, kChunkCols);
     }
     if (p.few && a.weigh) {
-        p.scores.cols = p.dec.cols;
+        p.scores.most = p.dec.cols;
+        p.scores.cols = (int)std::min<long>(p.dec.cols, (long)a.weigh * G);
         p.scores.pitch = (a.batch.max_kv + 127) / 128 * 128;
         const size_t n = (size_t)B * Hkv * p.scores.cols * p.scores.pitch * sizeof(float);
         p.keep_scores = n <= kMostScores;
@@ -473,7 +475,7 @@ hipError_t launch_paged_attn(const PagedAttn& a, bool e4m3, void* ws, hipStream_
         e = hipGetLastError();
         if (e != hipSuccess || !p.chunk) return e;
     }
-    const int min_cols = p.keep_scores ? p.scores.cols : 0;
+    const int min_cols = p.keep_scores ? p.scores.most : 0;
     auto go = [&](auto kern) { kern<<<dim3((a.batch.max_kv + kWeighKeys - 1) / kWeighKeys, a.kv.Hkv, a.batch.B), 256, 0, st>>>(a, min_cols); };
     if (D == 64) e4m3 ? go(paged_weigh_kernel<64, true>) : go(paged_weigh_kernel<64, false>);
     else if (D == 96) e4m3 ? go(paged_weigh_kernel<96, true>) : go(paged_weigh_kernel<96, false>);

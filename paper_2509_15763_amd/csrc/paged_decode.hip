@@ -192,10 +192,11 @@ __global__ __launch_bounds__(NT, NB == 1 && (FULL || D < 128 || E4M3) ? (D == 64
                 for (int t = 0; t < 4; ++t) odd |= E4M3 ? not_finite4(x.vw[j][t]) & 0x80808080u : not_finite2(x.vw[j][t]) & 0x80008000u;
         }
         if (scores.x) {  // base + 31 < pitch: base is a multiple of 32 below the entries, pitch one of 128 no smaller
+            const int skip = max(0, s.n - a.weigh) * G;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
-                if (16 * nb + r16 < ncol) {
-                    float* x = scores.x + (((size_t)b * a.kv.Hkv + hk) * scores.cols + 16 * nb + r16) * scores.pitch + base + 4 * g4;
+                if (16 * nb + r16 < ncol && 16 * nb + r16 >= skip) {
+                    float* x = scores.x + (((size_t)b * a.kv.Hkv + hk) * scores.cols + (16 * nb + r16 - skip)) * scores.pitch + base + 4 * g4;
 #pragma unroll
                     for (int kb = 0; kb < 2; ++kb) *(f32x4*)(x + 16 * kb) = sa[nb][kb] * c;
                 }

@@ -148,3 +148,12 @@ def test_more_workgroups_than_a_launch_takes():
     c = cache(n_pages=1 << 15, page=16, Hkv=51, D=8)
     assert size(c, B=65535, Hq=255, T=1 << 23, max_new=1 << 23, max_kv=1 << 23, weigh=0) == 0
     assert attn(c, B=65535, Hq=255, T=1 << 23, max_new=1 << 23, max_kv=1 << 23, weigh=0, hs=8, rs=8 * 255, out=FAKE + 4096) == EUNSUPPORTED
+
+
+@pytest.mark.parametrize("G", [1, 4, 8])
+def test_scores_are_kept_for_the_rows_that_count(G):
+    # one token of each counts: its G columns, where a chunk beside them makes room for 16
+    c = cache(n_pages=1 << 15, page=64, Hkv=8, D=128)
+    kw = dict(B=48, Hq=8 * G, T=48 + 63, max_new=64, max_kv=16384, W=1 << 23)
+    more = size(c, weigh=1, **kw) - size(c, weigh=0, **kw)
+    assert more == 48 * 8 * G * 16384 * 4
