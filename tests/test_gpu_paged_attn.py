@@ -478,3 +478,81 @@ def test_one_row_a_sequence_with_a_group_of_many_heads():
     wo, ll, _ = case.want(4, ALL)
     for x, y in ((out, lse), (want, wl)):
         assert out_ok(to_np(x), wo) and max_abs(to_np(y), ll) <= TOL_LSE_BF16
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("L", [6000, 20000])
+def test_a_chunk_in_dozens_of_slices(L, e4m3):
+    # four tiles over one kv head, cut into slices of 256 rows and more: 23 of them, or as many as there are at most (32)
+    case = Paged([L], [64], 64, 8, 1, 128, e4m3=e4m3, seed=27)
+    g = torch.Generator().manual_seed(28)
+    for h, j in enumerate((3, 700, L // 2, L - 2000, L - 900, L - 300, L - 70)):  # head h: a key that outweighs all others together in one slice
+        x = case.q[:, h].float().mean(0) + 0.3 * torch.randn(128, generator=g)
+        x = (x * 40 / x.norm()).to(torch.bfloat16)  # |x| = 40, |q| about 11
+        case.q[:, h] = (0.3 * case.q[:, h].float() + x.float() / 4).to(torch.bfloat16)  # scores of about 10 * 40 / 11 = 35
+        if e4m3:
+            x = torch.from_numpy(oracle.quantize_e4m3(x.float().numpy()[None, None, None], case.ks.numpy()))[0, 0, 0]
+        case.k[int(case.table[0, j // 64]), 0, j % 64] = x
+    check(case, 4, ALL)
+    check(case, 4, ALL, weigh=40, decay=0.5)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens,news", [([300, 1, 77, 1000], [1, 1, 1, 1]), ([700, 8, 64, 129], [8, 3, 5, 2]), ([700, 1, 64, 129], [33, 1, 5, 1])],
+                         ids=["tokens", "drafts", "with a chunk"])
+def test_weights_of_few_columns_without_kept_scores(lens, news, e4m3):
+    # a bound of 2^23 rows: the scores would take more than the workspace may, and are made a second time
+    import ctypes as C
+    case = Paged(lens, news, 16, 16, 2, 64, e4m3=e4m3, seed=29, missing=[(0, 2)])
+    c = case.cuda()
+    cache = u.binding._paged_cache(c.k, c.v, c.table, case.ks, case.vs, c.weight, values=False)
+    if e4m3:
+        cache.k_scale, cache.v_scale = c.ks.data_ptr(), c.vs.data_ptr()
+    size = lambda weigh: u.unigist_paged_attn_workspace(C.byref(cache), 4, 16, c.T, c.max_new, 1 << 23, 4, ALL * 2, 0, 0, weigh)
+    assert size(100) == size(0) > 0
+    wo, wl, added = case.want(4, 1 << 23, weigh=100)
+    out, lse = u.paged_attn(c.q.transpose(0, 1), c.k, c.v, c.table, c.kv_len, 4, 1 << 23, cu=c.cu, max_new=c.max_new, max_kv=1 << 23, weight=c.weight, weigh=100,
+                            decay=0.5, **c.scales)
+    want = case.want_weight(added, 0.5)
+    assert out_ok(to_np(out), wo) and max_abs(to_np(lse), wl) <= TOL_LSE_BF16
+    assert (np.abs(to_np(c.weight) - want) <= 2e-4 * want + 1e-9).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens,news", [([300, 150], [1, 1]), ([300, 150, 40], [1, 9, 20])], ids=["tokens", "two rows a tile"])
+def test_a_group_of_64_heads(lens, news, e4m3):
+    check(Paged(lens, news, 16, 64, 1, 128, e4m3=e4m3, seed=30), 4, ALL)
+    check(Paged(lens, news, 16, 64, 1, 128, e4m3=e4m3, seed=30), 4, 30, weigh=3, sinks=2)
+
+
+@pytest.mark.parametrize("news", [[1, 1], [3, 40], [300, 1]], ids=["decode", "drafts", "chunk"])
+def test_captured_and_replayed_with_other_tables(news):
+    # the pages move between the replays, and with them the weights
+    case = Paged([900, 500], news, 16, 8, 2, 128, seed=31)
+    c = case.cuda()
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    first = [x.clone() for x in (c.k, c.v, c.weight, c.table)]
+
+    def step():
+        return run(c, 4, ALL, weight=c.weight, weigh=2, decay=0.5, workspace=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        out, lse = step()
+    c.weight.copy_(first[2])
+    want = [x.clone() for x in step()]
+    weight = c.weight.clone()
+    for n in range(3):
+        to = torch.randperm(c.k.shape[0], generator=torch.Generator().manual_seed(n)).cuda()  # page p becomes page to[p]
+        for x, y in zip((c.k, c.v, c.weight), first):
+            x[to] = y
+        c.table.copy_(torch.where(first[3] >= 0, to[first[3].clamp(min=0).long()].int(), first[3]))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1]) and torch.equal(c.weight[to], weight), n

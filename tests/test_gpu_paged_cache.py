@@ -334,3 +334,46 @@ def test_append_of_as_many_rows_as_four_billion_threads():
     for h in range(Hkv):
         at = table[0].long()[rows // page]
         assert torch.equal(k[at, h, rows % page].view(torch.int16), new[h, rows].view(torch.int16))
+
+
+def test_evict_captured_and_replayed_with_other_tables():
+    # the pages move between the replays, on both sides
+    case = Paged([900, 500], [0, 0], 16, 2, 2, 64, seed=32)
+    c = case.cuda()
+    pool = c.k.shape[0]
+    ko, vo = (torch.zeros(60, 2, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    wo = torch.zeros(60, 2, 16, device="cuda")
+    to = torch.arange(60, dtype=torch.int32, device="cuda").view(2, 30)
+    keep = torch.tensor([300, 400], dtype=torch.int32, device="cuda")
+    first = [x.clone() for x in (c.k, c.v, c.weight, c.table)]
+
+    def step():
+        return u.paged_evict(c.k, c.v, c.table, c.kv_len, c.weight, keep, ko, vo, to, 900, 400, sinks=2, recent=5, weight_out=wo)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        rows, kept = step()
+    for x in (ko, vo, wo):
+        x.zero_()
+    r2, k2 = step()
+    want = [x.clone() for x in (ko.view(torch.int16), vo.view(torch.int16), wo)]
+    for n in range(3):
+        gen = torch.Generator().manual_seed(n)
+        move, out = torch.randperm(pool, generator=gen).cuda(), torch.randperm(60, generator=gen).cuda()
+        for x, y in zip((c.k, c.v, c.weight), first):
+            x[move] = y
+        c.table.copy_(torch.where(first[3] >= 0, move[first[3].clamp(min=0).long()].int(), first[3]))
+        to.copy_(out.int().view(2, 30))
+        for x in (ko, vo, wo):
+            x.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(rows, r2) and torch.equal(kept, k2)
+        for x, y in zip((ko.view(torch.int16), vo.view(torch.int16), wo), want):
+            assert torch.equal(x[out], y)
