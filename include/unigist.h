@@ -519,7 +519,8 @@ unigist_status unigist_paged_append(const unigist_paged_cache* cache, const void
  * window_mode (W >= max_kv in the sliding mode: plain causal attention), positions being row numbers.  A new row
  * that sees nothing gets out = 0 and lse = -inf; what invisible rows hold, infinities and NaN included, enters no result.
  * q, out: bf16, element (h, t, d) at h * q_head_stride + t * q_row_stride + d (as for append); lse [Hq, T] float, may be null.
- * out may be q itself where weigh = 0 (UNIGIST_EINVAL otherwise: the weights read q again), and shares no element with it else.
+ * The heads of a row are D elements or more apart.  out may be q itself where weigh = 0 (UNIGIST_EINVAL otherwise: the weights read
+ * q again), and shares no element with it else.
  * max_new >= every n[b] and max_kv >= every kv_len[b] choose the launch; rows of a sequence with more new ones may be left
  * unwritten.
  *

@@ -104,6 +104,7 @@ extern "C" unigist_status unigist_paged_attn(const unigist_paged_cache* c, const
     if (weigh > 0 && (!lse || !(decay >= 0.f) || isinf(decay))) return UNIGIST_EINVAL;
     if (T == 0) return UNIGIST_OK;
     if (!q || !out || !aligned16(q) || !aligned16(out)) return UNIGIST_EINVAL;
+    if (Hq > 1 && q_head_stride < c->D) return UNIGIST_EINVAL;  // heads of out on each other
     if (weigh > 0 && q == out) return UNIGIST_EINVAL;  // the weights are made from q once out is there
     if (q_head_stride % 8 != 0 || q_row_stride % 8 != 0 || q_row_stride < c->D || q_head_stride < 0) return UNIGIST_EINVAL;
     if (q_row_stride > 0x7fffffffLL) return UNIGIST_EUNSUPPORTED;

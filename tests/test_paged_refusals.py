@@ -157,3 +157,8 @@ def test_scores_are_kept_for_the_rows_that_count(G):
     kw = dict(B=48, Hq=8 * G, T=48 + 63, max_new=64, max_kv=16384, W=1 << 23)
     more = size(c, weigh=1, **kw) - size(c, weigh=0, **kw)
     assert more == 48 * 8 * G * 16384 * 4
+
+
+def test_heads_of_the_results_on_each_other():
+    for hs in (0, 56):
+        assert attn(hs=hs, out=FAKE + 4096) == EINVAL
