@@ -1334,6 +1334,8 @@ class PagedKVCache:
         x[B * cols + B:] = torch.tensor(cu, dtype=torch.int32)
         x = x.to(self.k.device)
         self.table, self.kv_len, self.cu = x[:B * cols].view(B, cols), x[B * cols:B * cols + B], x[B * cols + B:]
+        # rows that a mask has to show: the most of a renumbered sequence with new rows
+        self.whole = max((r for m, n, r in zip(self.renumbered, self.new, self.rows) if m and n), default=0)
 
     def extend(self, n):
         """n[b] more rows for sequence b; raises, and changes nothing, where a sequence outgrows its table or the pool its pages."""
@@ -1365,7 +1367,7 @@ class PagedKVCache:
         """q [Hq, sum(n), D], the queries of those rows -> out, lse.  Of a sequence that was evicted from, r, W, sinks and
         window_mode must show every row (W >= its rows, or as many sinks)."""
         self._enough("attend", q)
-        if any(m and x and max(int(W), int(sinks)) < n for m, x, n in zip(self.renumbered, self.new, self.rows)):
+        if max(int(W), int(sinks)) < self.whole:
             raise UnigistError("an evicted sequence's rows are renumbered: attend to all of them (W >= rows)")
         return paged_attn(q, self.k, self.v, self.table, self.kv_len, r, W, cu=self.cu, max_new=max(max(self.new), 1),
                           max_kv=max(max(self.rows), 1), sinks=sinks, window_mode=window_mode, k_scale=self.k_scale,
