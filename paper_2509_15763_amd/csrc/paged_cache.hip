@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedKv c, PagedBatch
 // that grows with the weight (the float's bits, made monotone; protected rows the largest, NaN the least); the keep-th
 // largest key is found digit by digit from histograms in LDS, then the rows above it and as many of those equal to it as are
 // left to take, lowest first, are numbered in row order.  Bound by latency: a thread holds the keys of PER rows, kSel apart, in
-// registers (all pages' numbers and then all weights in flight); sequences of more than PER * kSel rows are fetched again,
+// registers (two of 32 in scratch; all pages' numbers and then all weights in flight); sequences of more than PER * kSel rows are fetched again,
 // block by block, in each of the passes.  Rows are numbered from the counts of every 64 rows, scanned once.
 // 8 heads of 32768 rows 30 us (44.8 with the keys in LDS, eight in flight and a wave numbering a stretch of rows), 64 x 8 of 2304 16 (20.2).
 constexpr int kSel = 1024;  // threads
