@@ -483,8 +483,8 @@ unigist_status unigist_prefill_chunk_ragged(const void* q, const void* kc, const
  * are seen by no query and written by no call.  Sequences may share pages for reading; rows that a call writes
  * (unigist_paged_append, weights, the destination of unigist_paged_evict) belong to one sequence each.
  * weight: a number per row and kv head, of the caller's (null where it is not asked for).
- * k and v are 16-byte aligned, n_pages * Hkv * page is below 2^31 rows and at most 64 GiB each (UNIGIST_EUNSUPPORTED
- * otherwise).  The struct is read before a call returns.
+ * D is a multiple of 8 up to 128, of 16 for codes.  k and v are 16-byte aligned, n_pages * Hkv * page is below 2^31 rows
+ * and at most 64 GiB each (UNIGIST_EUNSUPPORTED otherwise).  The struct is read before a call returns.
  */
 typedef struct unigist_paged_cache {
     void* k;               /* DEVICE [n_pages, Hkv, page, D] */
@@ -544,8 +544,8 @@ size_t unigist_paged_attn_workspace(const unigist_paged_cache* cache, int B, int
  * the protected rows, the first `sinks` and the last `recent`, then the others by weight, largest first (NaN below
  * every number); of equal ones the lower row.  The rows of dst are numbered anew, for every kv head on its own: there row
  * numbers are no positions, and unigist_paged_attn is to be called with a window that holds every row (W >= max_kv).
- * dst: the same pool under another table, or another pool (any page size; Hkv, D and dt of src); its pages are none of
- * those that src's tables name.  src is left as it is.
+ * dst: the same pool under another table, or another pool (any page size; Hkv, D and dt of src, and its scales: codes are
+ * copied); its pages are none of those that src's tables name.  src is left as it is.
  * kv_len, keep: DEVICE, B ints, kv_len[b] <= max_kv, keep[b] <= max_keep.  kept (DEVICE [B, Hkv, max_keep], out): the rows
  * kept, ascending, then -1.  rows_out (DEVICE, B ints, out; not kv_len's or keep's memory): rows kept, or -1 for a
  * sequence whose numbers are outside those bounds or that misses a page on either side; nothing is copied for it and
